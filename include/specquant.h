@@ -77,6 +77,7 @@ typedef enum { SQ_ACCEPT_SAMPLE = 0, SQ_ACCEPT_GREEDY = 1 } sq_accept_mode;
 #define SQ_DEV_NONFINITE_LOGIT  0x20u /* a logit row held inf or NaN         */
 #define SQ_DEV_BAD_POSITION     0x40u /* a token position outside the cache  */
 #define SQ_DEV_BAD_TOKEN_ID     0x80u /* an embedding id outside [0, V)      */
+#define SQ_DEV_NONFINITE_KV    0x100u /* sq_kv4_append: inf or NaN in a row  */
 
 /* Thread-local text of the last error raised on this host thread. */
 SQ_API const char* sq_last_error(void);
@@ -411,6 +412,108 @@ SQ_API sq_status sq_spec_commit(const int32_t* n_accepted, const int32_t* tokens
                                 sq_stream_t stream);
 SQ_API sq_status sq_spec_drafts(const int32_t* samples, const int32_t* last2, int B, int K,
                                 int32_t* verify_tokens, int32_t* draft, sq_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Whole prompts (Sec. III-D: every model of the method first reads the
+ * prompt; the paper gives no model internals).
+ *
+ * sq_attention_prompt: attention of a packed batch of prompts of different
+ * lengths, with the append of their keys and values.  qkv fp16
+ * [N, (Hq + 2 Hkv) * D] as for sq_attention, but row offsets[b] + t is token
+ * t of sequence b, t < offsets[b+1] - offsets[b] (offsets int32 [B+1],
+ * device, 0 <= offsets[0] <= .. <= offsets[B] <= N; sequences may be empty;
+ * rows that belong to none, as behind the last, are not read and their rows
+ * of out stay as they are).  Token t is at position pos0[b] + t: pos0 > 0
+ * continues behind a cached prefix.  The rotated key and the value of every
+ * token go to the fp16 caches [B, Hkv, max_ctx, D] at its position; then
+ *   out[row] = sum_{j <= pos} p_j v_j / sum_j p_j,
+ *   p_j = exp(q . k_j / sqrt(D))
+ * over the cache, query head h against key/value head h / (Hq / Hkv), out
+ * fp16 [N, Hq * D].  Rotated queries and keys are rounded to fp16 once,
+ * correctly; products are exact; sums and the softmax's statistics are fp32;
+ * a probability relative to its row's maximum is rounded to fp16 for its
+ * product with the value (its sum is not).  What lies in the caches behind a
+ * token's position, infinities and NaN included, has no effect on its row;
+ * scores of -inf have no weight, and a row without any other is zero.  A sequence
+ * that does not fit its cache (pos0[b] < 0 or pos0[b] + length > max_ctx)
+ * writes nothing to it, gets zero rows and sets SQ_DEV_BAD_POSITION; offsets
+ * that decrease or leave [0, N] set it too, and nothing at all is written.
+ * Limits: D = 128, Hq / Hkv <= 256, B <= 65535, N <= 2^22, N * Hq <= 2^30,
+ * max_ctx <= 2^17.  qkv, caches and out 16-byte aligned.  workspace:
+ * sq_attention_prompt_workspace_bytes(...) bytes, 16-byte aligned, no
+ * zero-fill needed; calls sharing one must not overlap on the GPU. */
+SQ_API size_t sq_attention_prompt_workspace_bytes(int B, int64_t N, int Hq, int Hkv, int D, int64_t max_ctx);
+SQ_API sq_status sq_attention_prompt(const void* qkv, int64_t N, const int32_t* offsets, int B, int Hq, int Hkv,
+                                     int D, const int32_t* pos0, float theta, void* k_cache, void* v_cache,
+                                     int64_t max_ctx, void* out, void* workspace, size_t ws_bytes,
+                                     sq_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * The key/value cache in four bits (Sec. III-A keeps the variants' weights in
+ * 4 and 8 bits; the paper leaves the caches open).  A row is one position of
+ * one key/value head: 128 fp16 values x, of a key after its rotation, which
+ * is rounded to fp16 once, correctly.  With lo = min x and hi = max x,
+ *   s = fp16((hi - lo) / 15), 2^-24 if that is zero and hi > lo,
+ *   c = clamp(rint((x - lo) / s), 0, 15) (ties to even), 0 if s = 0,
+ * every step rounded to fp32; the row stands for c * s + lo.  Codes and
+ * parameters are bit-identical to this definition.
+ *   k_codes  uint8 [B, Hkv, max_ctx, 64]: byte i holds dimension 2i in its
+ *            low half and 2i + 1 in its high half
+ *   v_codes  uint8 [B, Hkv, max_ctx / 2, 128]: per pair of positions, bytes
+ *            4i, 4i + 1 hold dimensions 4i .. 4i + 3 of the even position
+ *            (low halves first), bytes 4i + 2, 4i + 3 those of the odd one
+ *   k_params, v_params  fp16 [B, Hkv, max_ctx, 2]: (s, lo)
+ * 136 bytes a position and head for both against 512 in fp16.  All four
+ * 16-byte aligned; max_ctx a multiple of 16.
+ *
+ * sq_kv4_append: the new tokens' rows into the caches; qkv, offsets and pos0
+ *   as for sq_attention_prompt, or offsets NULL: N / B tokens of each
+ *   sequence, rows b * (N / B) + t.  A row with inf or NaN (a rotated key
+ *   beyond fp16's range counts) is kept as (NaN, NaN), reads as NaN and sets
+ *   SQ_DEV_NONFINITE_KV.  Sequences that do not fit, and bad offsets, write
+ *   nothing and set SQ_DEV_BAD_POSITION.
+ * sq_kv4_unpack: fp16(c * s + lo) of positions first[b] <= j < last[b] into
+ *   fp16 caches [B, Hkv, max_ctx, D] (first, last int32 [B], device; other
+ *   positions stay as they are): the prefix that sq_attention_prompt
+ *   continues behind.  first[b] < 0 or last[b] > max_ctx (and first < last)
+ *   writes nothing for b and sets SQ_DEV_BAD_POSITION.
+ * sq_attention_kv4: sq_attention over these caches (same arguments, layouts
+ *   and limits; the new tokens already appended): fp32 accumulation over
+ *   exact codes, out fp16.  Rows behind a query's position have no effect,
+ *   whatever they hold.  A sequence with pos0[b] < 0 or pos0[b] + T > max_ctx
+ *   gets zero rows and sets SQ_DEV_BAD_POSITION.  workspace:
+ *   sq_attention_kv4_workspace_bytes(...) bytes, 16-byte aligned, no
+ *   zero-fill; calls sharing one must not overlap on the GPU. */
+SQ_API sq_status sq_kv4_append(const void* qkv, int64_t N, const int32_t* offsets, int B, int Hq, int Hkv, int D,
+                               const int32_t* pos0, float theta, void* k_codes, void* k_params, void* v_codes,
+                               void* v_params, int64_t max_ctx, sq_stream_t stream);
+SQ_API sq_status sq_kv4_unpack(const void* k_codes, const void* k_params, const void* v_codes,
+                               const void* v_params, int B, int Hkv, int D, int64_t max_ctx,
+                               const int32_t* first, const int32_t* last, void* k_cache, void* v_cache,
+                               sq_stream_t stream);
+SQ_API size_t sq_attention_kv4_workspace_bytes(int B, int T, int Hq, int Hkv, int D, int64_t max_ctx);
+SQ_API sq_status sq_attention_kv4(const void* qkv, int B, int T, int Hq, int Hkv, int D, const int32_t* pos0,
+                                  float theta, const void* k_codes, const void* k_params, const void* v_codes,
+                                  const void* v_params, int64_t max_ctx, void* out, void* workspace,
+                                  size_t ws_bytes, sq_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * sq_logprobs: what a program answers beside its tokens, or scores a prompt
+ * by.  For each of R rows of fp16 logits z [R, V], x_v = (z_v - max z) / T:
+ *   logprob[r]  = x_t - log sum_v e^(x_v) of t = tokens[r]  (fp32; tokens
+ *                 int32 [R] and logprob both given, or both NULL)
+ *   entropy[r]  = -sum_v p_v log p_v in nats  (fp32 [R], or NULL)
+ *   top_tokens, top_logprobs [R, top]: the `top` entries of the largest
+ *                 logits, largest first, the lowest index among equals, and
+ *                 their log probabilities (0 <= top <= 32, top <= V)
+ * fp32 arithmetic, one launch, no workspace.  A logit of -inf is an entry
+ * without probability (a banned token): its logprob is -inf.  A row with NaN
+ * or +inf, or with nothing but -inf, gives NaN and top_tokens -1 and sets
+ * SQ_DEV_NONFINITE_LOGIT or SQ_DEV_NO_MASS; a token outside [0, V) gives NaN
+ * and sets SQ_DEV_BAD_TOKEN_ID.  R <= 2^24, V < 2^20; z 2-byte aligned. */
+SQ_API sq_status sq_logprobs(const void* z, int64_t R, int64_t V, float temperature, const int32_t* tokens,
+                             float* logprob, float* entropy, int top, int32_t* top_tokens, float* top_logprobs,
+                             sq_stream_t stream);
 
 /* ------------------------------------------------------------------------
  * sq_accept_noalloc: sq_accept without a caller workspace.  The paper has

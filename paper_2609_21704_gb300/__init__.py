@@ -32,6 +32,8 @@ __all__ = [
     "sq_softmax_workspace_bytes", "sq_softmax", "sq_rmsnorm", "sq_kv_append",
     "sq_attention_workspace_bytes", "sq_attention", "sq_kv_rollback", "sq_embed",
     "sq_attention_append", "sq_linear_norm", "sq_spec_commit", "sq_spec_drafts",
+    "sq_attention_prompt_workspace_bytes", "sq_attention_prompt", "sq_kv4_append", "sq_kv4_unpack",
+    "sq_attention_kv4_workspace_bytes", "sq_attention_kv4", "sq_logprobs",
     "EXPORTED_SYMBOLS",
 ]
 
@@ -42,6 +44,7 @@ SQ_EPI_NONE, SQ_EPI_SILU_GATE, SQ_EPI_RESIDUAL = 0, 1, 2
 SQ_W_FP16, SQ_W_INT4, SQ_W_FP8 = 0, 1, 2
 SQ_DEV_NONFINITE_WEIGHT, SQ_DEV_BAD_DRAFT_TOKEN, SQ_DEV_NO_MASS, SQ_DEV_BAD_UNIFORM = 1, 2, 4, 8
 SQ_DEV_TIMEOUT, SQ_DEV_NONFINITE_LOGIT, SQ_DEV_BAD_POSITION, SQ_DEV_BAD_TOKEN_ID = 0x10, 0x20, 0x40, 0x80
+SQ_DEV_NONFINITE_KV = 0x100
 
 _P = ctypes.c_void_p
 _I64 = ctypes.c_int64
@@ -84,6 +87,15 @@ _SIGS = {
                                    _P, _SIZE, _P]),
     "sq_spec_commit": (_INT, [_P, _P, _INT, _INT, _INT, _P, _INT, _P, _P, _P, _P]),
     "sq_spec_drafts": (_INT, [_P, _P, _INT, _INT, _P, _P, _P]),
+    "sq_attention_prompt_workspace_bytes": (_SIZE, [_INT, _I64, _INT, _INT, _INT, _I64]),
+    "sq_attention_prompt": (_INT, [_P, _I64, _P, _INT, _INT, _INT, _INT, _P, ctypes.c_float, _P, _P, _I64, _P,
+                                   _P, _SIZE, _P]),
+    "sq_kv4_append": (_INT, [_P, _I64, _P, _INT, _INT, _INT, _INT, _P, ctypes.c_float, _P, _P, _P, _P, _I64, _P]),
+    "sq_kv4_unpack": (_INT, [_P, _P, _P, _P, _INT, _INT, _INT, _I64, _P, _P, _P, _P, _P]),
+    "sq_attention_kv4_workspace_bytes": (_SIZE, [_INT, _INT, _INT, _INT, _INT, _I64]),
+    "sq_attention_kv4": (_INT, [_P, _INT, _INT, _INT, _INT, _INT, _P, ctypes.c_float, _P, _P, _P, _P, _I64, _P,
+                                _P, _SIZE, _P]),
+    "sq_logprobs": (_INT, [_P, _I64, _I64, ctypes.c_float, _P, _P, _P, _INT, _P, _P, _P]),
 }
 EXPORTED_SYMBOLS = tuple(_SIGS)
 
@@ -336,6 +348,123 @@ def sq_spec_drafts(samples, last2, verify_tokens, draft, stream=None) -> None:
     B, K1 = verify_tokens.shape
     _check("sq_spec_drafts", load().sq_spec_drafts(_ptr(samples), _ptr(last2), B, K1 - 1,
                                                    _ptr(verify_tokens), _ptr(draft), _stream(stream)))
+
+
+def _want(what: str, t, dtype, *shape):
+    """t is a tensor of this type and shape (None: any size) on the current device."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{what}: expected a torch.Tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{what}: expected {dtype}, got {t.dtype}")
+    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise ValueError(f"{what}: expected shape {shape}, got {tuple(t.shape)}")
+    if t.is_cuda and t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what}: on {t.device}, but the current device is {torch.cuda.current_device()}")
+    return t
+
+
+def sq_attention_prompt_workspace_bytes(B, N, Hq, Hkv, max_ctx) -> int:
+    return int(load().sq_attention_prompt_workspace_bytes(B, N, Hq, Hkv, 128, max_ctx))
+
+
+def _heads(qkv, Hq, Hkv):
+    if Hq < 1 or Hkv < 1 or Hq % Hkv:
+        raise ValueError(f"Hq = {Hq} must be a positive multiple of Hkv = {Hkv}")
+    return _want("qkv", qkv, torch.float16, None, (Hq + 2 * Hkv) * 128).shape[0]
+
+
+def sq_attention_prompt(qkv, offsets, Hq, Hkv, pos0, theta, k_cache, v_cache, out, workspace,
+                        stream=None) -> None:
+    """Causal GQA attention of packed prompts and the append of their keys and
+    values: qkv fp16 [N, (Hq+2Hkv)*128], offsets int32 [B+1] (sequence b: rows
+    offsets[b] .. offsets[b+1]-1, at positions pos0[b] ..), caches fp16
+    [B, Hkv, max_ctx, 128], out fp16 [N, Hq*128]."""
+    N = _heads(qkv, Hq, Hkv)
+    B = _want("pos0", pos0, torch.int32, None).shape[0]
+    _want("offsets", offsets, torch.int32, B + 1)
+    C = _want("k_cache", k_cache, torch.float16, B, Hkv, None, 128).shape[2]
+    _want("v_cache", v_cache, torch.float16, B, Hkv, C, 128)
+    _want("out", out, torch.float16, N, Hq * 128)
+    _check("sq_attention_prompt", load().sq_attention_prompt(
+        _ptr(qkv), N, _ptr(offsets), B, Hq, Hkv, 128, _ptr(pos0), float(theta), _ptr(k_cache), _ptr(v_cache), C,
+        _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def _kv4(B, Hkv, k_codes, k_params, v_codes, v_params):
+    C = _want("k_codes", k_codes, torch.uint8, B, Hkv, None, 64).shape[2]
+    _want("k_params", k_params, torch.float16, B, Hkv, C, 2)
+    if v_codes.numel() != k_codes.numel():
+        raise ValueError(f"v_codes: expected {k_codes.numel()} bytes, got {v_codes.numel()}")
+    _want("v_codes", v_codes, torch.uint8, *v_codes.shape)
+    _want("v_params", v_params, torch.float16, B, Hkv, C, 2)
+    return C, (_ptr(k_codes), _ptr(k_params), _ptr(v_codes), _ptr(v_params))
+
+
+def sq_kv4_append(qkv, Hq, Hkv, pos0, theta, k_codes, k_params, v_codes, v_params, offsets=None,
+                  stream=None) -> None:
+    """The new tokens' keys (rotated) and values into the 4-bit caches: codes
+    uint8 [B, Hkv, max_ctx, 64] (v_codes in pairs of positions, see the C
+    declaration), params fp16 [B, Hkv, max_ctx, 2]; rows of qkv as for
+    sq_attention_prompt, or without offsets N / B of each sequence."""
+    N = _heads(qkv, Hq, Hkv)
+    B = _want("pos0", pos0, torch.int32, None).shape[0]
+    if offsets is not None:
+        _want("offsets", offsets, torch.int32, B + 1)
+    C, ptrs = _kv4(B, Hkv, k_codes, k_params, v_codes, v_params)
+    _check("sq_kv4_append", load().sq_kv4_append(_ptr(qkv), N, _ptr(offsets), B, Hq, Hkv, 128, _ptr(pos0),
+                                                 float(theta), *ptrs, C, _stream(stream)))
+
+
+def sq_kv4_unpack(k_codes, k_params, v_codes, v_params, first, last, k_cache, v_cache, stream=None) -> None:
+    """Positions first[b] .. last[b]-1 of the 4-bit caches as fp16 into
+    k_cache, v_cache [B, Hkv, max_ctx, 128]."""
+    B = _want("first", first, torch.int32, None).shape[0]
+    _want("last", last, torch.int32, B)
+    Hkv = _want("k_cache", k_cache, torch.float16, B, None, None, 128).shape[1]
+    C, ptrs = _kv4(B, Hkv, k_codes, k_params, v_codes, v_params)
+    _want("k_cache", k_cache, torch.float16, B, Hkv, C, 128)
+    _want("v_cache", v_cache, torch.float16, B, Hkv, C, 128)
+    _check("sq_kv4_unpack", load().sq_kv4_unpack(*ptrs, B, Hkv, 128, C, _ptr(first), _ptr(last), _ptr(k_cache),
+                                                 _ptr(v_cache), _stream(stream)))
+
+
+def sq_attention_kv4_workspace_bytes(B, T, Hq, Hkv, max_ctx) -> int:
+    return int(load().sq_attention_kv4_workspace_bytes(B, T, Hq, Hkv, 128, max_ctx))
+
+
+def sq_attention_kv4(qkv, B, T, Hq, Hkv, pos0, theta, k_codes, k_params, v_codes, v_params, out, workspace,
+                     stream=None) -> None:
+    """out fp16 [B*T, Hq*128] = causal GQA attention of T new tokens a sequence
+    (already appended) over the 4-bit caches."""
+    if _heads(qkv, Hq, Hkv) != B * T:
+        raise ValueError(f"qkv: expected {B * T} rows, got {qkv.shape[0]}")
+    _want("pos0", pos0, torch.int32, B)
+    C, ptrs = _kv4(B, Hkv, k_codes, k_params, v_codes, v_params)
+    _want("out", out, torch.float16, B * T, Hq * 128)
+    _check("sq_attention_kv4", load().sq_attention_kv4(
+        _ptr(qkv), B, T, Hq, Hkv, 128, _ptr(pos0), float(theta), *ptrs, C, _ptr(out), _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def sq_logprobs(z, temperature, tokens=None, logprob=None, entropy=None, top_tokens=None, top_logprobs=None,
+                stream=None) -> None:
+    """Rows of fp16 logits z [R, V]: logprob fp32 [R] of tokens int32 [R], the
+    entropy fp32 [R], and the largest entries' top_tokens int32 [R, top] and
+    top_logprobs fp32 [R, top]; what is None is left out."""
+    R, V = _want("z", z, torch.float16, None, None).shape
+    if tokens is not None:
+        _want("tokens", tokens, torch.int32, R)
+    for what, t in (("logprob", logprob), ("entropy", entropy)):
+        if t is not None:
+            _want(what, t, torch.float32, R)
+    top = 0
+    if top_tokens is not None:
+        top = _want("top_tokens", top_tokens, torch.int32, R, None).shape[1]
+    if top_logprobs is not None or top:
+        _want("top_logprobs", top_logprobs, torch.float32, R, top)
+    _check("sq_logprobs", load().sq_logprobs(_ptr(z), R, V, float(temperature), _ptr(tokens), _ptr(logprob),
+                                             _ptr(entropy), top, _ptr(top_tokens) if top else None,
+                                             _ptr(top_logprobs) if top else None, _stream(stream)))
 
 
 def sq_accept_workspace_bytes(B: int, K: int, V: int) -> int:

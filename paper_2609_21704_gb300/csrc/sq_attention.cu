@@ -26,7 +26,6 @@ namespace sq {
 
 __device__ unsigned int g_attn_status;
 
-constexpr int kHeadDim = 128;
 constexpr int kAttnWarps = 4;
 constexpr int kAttnThreads = 32 * kAttnWarps;
 constexpr int kMaxT = 32;           // new tokens per sequence and call
@@ -76,15 +75,6 @@ __global__ void __launch_bounds__(256) rmsnorm_kernel(const __half* __restrict__
 }
 
 // ---- RoPE --------------------------------------------------------------------
-// Inverse frequencies theta^(-2d/D), d < D/2, as turns per position in units
-// of 2^-64 of a turn: pos * f modulo 2^64 is the angle modulo 2 pi without
-// any fp64 arithmetic (two fp64 operations per clock and SM on this GPU: the
-// T positions' table cost 2 us per CTA at T = 28).  f comes from fp64, so
-// positions up to 2^17 keep the angle within 1e-10, as an fp64 reduction would.
-struct RopeFreq {
-  unsigned long long f[kHeadDim / 2];
-};
-
 // cos and sin of the angle at `pos`: the turn as a signed fraction a + b of
 // 2^64 (24 leading bits, and the rest), times 2 pi in fp32 (head and tail of
 // the constant, one rounding of the angle), then fp32 sincosf.
@@ -806,7 +796,7 @@ cudaError_t launch_rmsnorm(const __half* x, const __half* gamma, int M, int64_t 
   return launch_pdl(rmsnorm_kernel, dim3((unsigned)M), dim3(256), 0, st, x, gamma, H, eps, y);
 }
 
-static RopeFreq rope_freq(double theta) {
+RopeFreq rope_freq(double theta) {
   // the last theta's table per host thread (64 pow calls take longer than a launch)
   static thread_local double last = 0.0;
   static thread_local RopeFreq rf;

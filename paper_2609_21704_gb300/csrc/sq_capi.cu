@@ -12,6 +12,7 @@
 
 #include "sq_decoder.h"
 #include "sq_internal.h"
+#include "sq_serve.h"
 
 namespace sq {
 
@@ -81,6 +82,9 @@ sq_status sq_check(sq_stream_t stream, uint32_t* device_bits) {
       (e = take_gemv_status_fp16(&bits)) != cudaSuccess || (e = take_tc_status(&bits)) != cudaSuccess ||
       (e = take_attn_status(&bits)) != cudaSuccess || (e = take_ring_status(&bits)) != cudaSuccess)
     return cuda_fail(e, "sq_check: linear status");
+  if ((e = take_prompt_status(&bits)) != cudaSuccess || (e = take_kv4_status(&bits)) != cudaSuccess ||
+      (e = take_logprobs_status(&bits)) != cudaSuccess)
+    return cuda_fail(e, "sq_check: prompt, cache or log probability status");
   if (device_bits) *device_bits = bits;
   if (bits) return fail(SQ_ERR_DEVICE, "sq_check: device status bits 0x%x", bits);
   return SQ_OK;
@@ -655,6 +659,190 @@ sq_status sq_spec_drafts(const int32_t* samples, const int32_t* last2, int B, in
     return fail(SQ_ERR_ALIGN, "sq_spec_drafts: pointers must be 4-byte aligned");
   cudaError_t e = launch_spec_drafts(samples, last2, B, K, verify_tokens, draft, (cudaStream_t)stream);
   if (e != cudaSuccess) return cuda_fail(e, "sq_spec_drafts: launch");
+  return SQ_OK;
+}
+
+// ---- prompt attention, the 4-bit cache, log probabilities
+
+// Head layout and cache length of the calls below.
+static sq_status check_heads(const char* who, int B, int Hq, int Hkv, int D, float theta, int64_t max_ctx) {
+  if (B < 0 || B > 65535 || Hq < 1 || Hkv < 1 || Hq % Hkv || Hq / Hkv > 256 || Hq > 65535)
+    return fail(SQ_ERR_SHAPE, "%s: need 0 <= B <= 65535, Hq a positive multiple of Hkv, Hq / Hkv <= 256 (B=%d "
+                "Hq=%d Hkv=%d)", who, B, Hq, Hkv);
+  if (D != 128) return fail(SQ_ERR_UNSUPPORTED, "%s: head dimension %d (only 128 is built)", who, D);
+  if (max_ctx < 1 || max_ctx > kPromptMaxCtx)
+    return fail(SQ_ERR_SHAPE, "%s: need 1 <= max_ctx <= 2^17 (max_ctx=%lld)", who, (long long)max_ctx);
+  if ((int64_t)B * Hkv > ((int64_t)1 << 20)) return fail(SQ_ERR_SHAPE, "%s: B * Hkv > 2^20", who);
+  if (!(theta > 1.0f) || !std::isfinite(theta)) return fail(SQ_ERR_INVALID_ARG, "%s: theta must be > 1", who);
+  return SQ_OK;
+}
+
+static sq_status check_rows(const char* who, int64_t N, int Hq) {
+  if (N < 0 || N > ((int64_t)1 << 22) || N * Hq > ((int64_t)1 << 30))
+    return fail(SQ_ERR_SHAPE, "%s: need 0 <= rows <= 2^22 and rows * Hq <= 2^30 (rows=%lld)", who, (long long)N);
+  return SQ_OK;
+}
+
+size_t sq_attention_prompt_workspace_bytes(int B, int64_t N, int Hq, int Hkv, int D, int64_t max_ctx) {
+  if (check_heads("sq_attention_prompt_workspace_bytes", B, Hq, Hkv, D, 2.0f, max_ctx) != SQ_OK ||
+      check_rows("sq_attention_prompt_workspace_bytes", N, Hq) != SQ_OK)
+    return 0;
+  return prompt_workspace_bytes(B, N, Hq, Hkv, max_ctx);
+}
+
+sq_status sq_attention_prompt(const void* qkv, int64_t N, const int32_t* offsets, int B, int Hq, int Hkv, int D,
+                              const int32_t* pos0, float theta, void* k_cache, void* v_cache, int64_t max_ctx,
+                              void* out, void* workspace, size_t ws_bytes, sq_stream_t stream) {
+  SQ_RANGE();
+  const char* who = "sq_attention_prompt";
+  sq_status st = check_heads(who, B, Hq, Hkv, D, theta, max_ctx);
+  if (st != SQ_OK || (st = check_rows(who, N, Hq)) != SQ_OK) return st;
+  if (B == 0 || N == 0) return SQ_OK;
+  if (!qkv || !offsets || !pos0 || !k_cache || !v_cache || !out)
+    return fail(SQ_ERR_INVALID_ARG, "%s: NULL pointer", who);
+  if (!aligned(qkv, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(out, 16))
+    return fail(SQ_ERR_ALIGN, "%s: qkv, caches and out must be 16-byte aligned", who);
+  if (!aligned(offsets, 4) || !aligned(pos0, 4)) return fail(SQ_ERR_ALIGN, "%s: misaligned pointer", who);
+  if (out == qkv || k_cache == v_cache) return fail(SQ_ERR_INVALID_ARG, "%s: out and the caches must not alias", who);
+  const size_t need = prompt_workspace_bytes(B, N, Hq, Hkv, max_ctx);
+  if (!workspace || ws_bytes < need)
+    return fail(SQ_ERR_WORKSPACE, "%s: workspace %zu bytes < %zu required", who, ws_bytes, need);
+  if (!aligned(workspace, 16)) return fail(SQ_ERR_ALIGN, "%s: workspace must be 16-byte aligned", who);
+  const Packed pk = {offsets, pos0, B, 0, N, max_ctx};
+  cudaError_t e = launch_prompt(reinterpret_cast<const __half*>(qkv), pk, Hq, Hkv, (double)theta,
+                                reinterpret_cast<__half*>(k_cache), reinterpret_cast<__half*>(v_cache),
+                                reinterpret_cast<__half*>(out), workspace, (cudaStream_t)stream);
+  if (e != cudaSuccess) return cuda_fail(e, who);
+  return SQ_OK;
+}
+
+static sq_status check_kv4(const char* who, const void* kc, const void* kp, const void* vc, const void* vp,
+                           int64_t max_ctx) {
+  if (max_ctx % 16) return fail(SQ_ERR_SHAPE, "%s: max_ctx must be a multiple of 16 (max_ctx=%lld)", who,
+                                (long long)max_ctx);
+  if (!kc || !kp || !vc || !vp) return fail(SQ_ERR_INVALID_ARG, "%s: NULL cache pointer", who);
+  if (!aligned(kc, 16) || !aligned(kp, 16) || !aligned(vc, 16) || !aligned(vp, 16))
+    return fail(SQ_ERR_ALIGN, "%s: caches must be 16-byte aligned", who);
+  if (kc == vc || kp == vp) return fail(SQ_ERR_INVALID_ARG, "%s: keys and values must not share a cache", who);
+  return SQ_OK;
+}
+
+static KV4Cache kv4_cache(const void* kc, const void* kp, const void* vc, const void* vp) {
+  KV4Cache c;
+  c.kc = reinterpret_cast<uint8_t*>(const_cast<void*>(kc));
+  c.kp = reinterpret_cast<__half*>(const_cast<void*>(kp));
+  c.vc = reinterpret_cast<uint8_t*>(const_cast<void*>(vc));
+  c.vp = reinterpret_cast<__half*>(const_cast<void*>(vp));
+  return c;
+}
+
+sq_status sq_kv4_append(const void* qkv, int64_t N, const int32_t* offsets, int B, int Hq, int Hkv, int D,
+                        const int32_t* pos0, float theta, void* k_codes, void* k_params, void* v_codes,
+                        void* v_params, int64_t max_ctx, sq_stream_t stream) {
+  SQ_RANGE();
+  const char* who = "sq_kv4_append";
+  sq_status st = check_heads(who, B, Hq, Hkv, D, theta, max_ctx);
+  if (st != SQ_OK || (st = check_rows(who, N, Hq)) != SQ_OK) return st;
+  if (!offsets && B > 0 && N % B)
+    return fail(SQ_ERR_SHAPE, "%s: without offsets the rows must be a multiple of B (rows=%lld B=%d)", who,
+                (long long)N, B);
+  if (B == 0 || N == 0) return SQ_OK;
+  if (!qkv || !pos0) return fail(SQ_ERR_INVALID_ARG, "%s: NULL pointer", who);
+  if (!aligned(qkv, 16) || !aligned(offsets, 4) || !aligned(pos0, 4))
+    return fail(SQ_ERR_ALIGN, "%s: misaligned pointer (qkv needs 16 bytes)", who);
+  if ((st = check_kv4(who, k_codes, k_params, v_codes, v_params, max_ctx)) != SQ_OK) return st;
+  const Packed pk = {offsets, pos0, B, offsets ? 0 : (int)(N / B), N, max_ctx};
+  cudaError_t e = launch_kv4_append(reinterpret_cast<const __half*>(qkv), pk, Hq, Hkv, (double)theta,
+                                    kv4_cache(k_codes, k_params, v_codes, v_params), (cudaStream_t)stream);
+  if (e != cudaSuccess) return cuda_fail(e, who);
+  return SQ_OK;
+}
+
+sq_status sq_kv4_unpack(const void* k_codes, const void* k_params, const void* v_codes, const void* v_params,
+                        int B, int Hkv, int D, int64_t max_ctx, const int32_t* first, const int32_t* last,
+                        void* k_cache, void* v_cache, sq_stream_t stream) {
+  SQ_RANGE();
+  const char* who = "sq_kv4_unpack";
+  sq_status st = check_heads(who, B, Hkv, Hkv, D, 2.0f, max_ctx);
+  if (st != SQ_OK) return st;
+  if (B == 0) return SQ_OK;
+  if (!first || !last || !k_cache || !v_cache) return fail(SQ_ERR_INVALID_ARG, "%s: NULL pointer", who);
+  if (!aligned(first, 4) || !aligned(last, 4) || !aligned(k_cache, 16) || !aligned(v_cache, 16))
+    return fail(SQ_ERR_ALIGN, "%s: misaligned pointer (caches need 16 bytes)", who);
+  if (k_cache == v_cache) return fail(SQ_ERR_INVALID_ARG, "%s: keys and values must not share a cache", who);
+  if ((st = check_kv4(who, k_codes, k_params, v_codes, v_params, max_ctx)) != SQ_OK) return st;
+  cudaError_t e = launch_kv4_unpack(kv4_cache(k_codes, k_params, v_codes, v_params), B, Hkv, max_ctx, first, last,
+                                    reinterpret_cast<__half*>(k_cache), reinterpret_cast<__half*>(v_cache),
+                                    (cudaStream_t)stream);
+  if (e != cudaSuccess) return cuda_fail(e, who);
+  return SQ_OK;
+}
+
+static sq_status check_kv4_tokens(const char* who, int T, int Hq, int Hkv) {
+  if (T < 0 || T > attention_max_tokens() || (int64_t)(Hq / Hkv) * T > 200)
+    return fail(SQ_ERR_SHAPE, "%s: need 0 <= T <= %d and (Hq / Hkv) * T <= 200 (T=%d)", who,
+                attention_max_tokens(), T);
+  return SQ_OK;
+}
+
+size_t sq_attention_kv4_workspace_bytes(int B, int T, int Hq, int Hkv, int D, int64_t max_ctx) {
+  if (check_heads("sq_attention_kv4_workspace_bytes", B, Hq, Hkv, D, 2.0f, max_ctx) != SQ_OK ||
+      check_kv4_tokens("sq_attention_kv4_workspace_bytes", T, Hq, Hkv) != SQ_OK)
+    return 0;
+  return attention_kv4_workspace_bytes(B, T, Hq, Hkv, max_ctx);
+}
+
+sq_status sq_attention_kv4(const void* qkv, int B, int T, int Hq, int Hkv, int D, const int32_t* pos0,
+                           float theta, const void* k_codes, const void* k_params, const void* v_codes,
+                           const void* v_params, int64_t max_ctx, void* out, void* workspace, size_t ws_bytes,
+                           sq_stream_t stream) {
+  SQ_RANGE();
+  const char* who = "sq_attention_kv4";
+  sq_status st = check_heads(who, B, Hq, Hkv, D, theta, max_ctx);
+  if (st != SQ_OK || (st = check_kv4_tokens(who, T, Hq, Hkv)) != SQ_OK) return st;
+  if (B == 0 || T == 0) return SQ_OK;
+  if (!qkv || !pos0 || !out) return fail(SQ_ERR_INVALID_ARG, "%s: NULL pointer", who);
+  if (!aligned(qkv, 16) || !aligned(out, 16) || !aligned(pos0, 4))
+    return fail(SQ_ERR_ALIGN, "%s: misaligned pointer (qkv and out need 16 bytes)", who);
+  if (out == qkv) return fail(SQ_ERR_INVALID_ARG, "%s: out must not alias qkv", who);
+  if ((st = check_kv4(who, k_codes, k_params, v_codes, v_params, max_ctx)) != SQ_OK) return st;
+  const size_t need = attention_kv4_workspace_bytes(B, T, Hq, Hkv, max_ctx);
+  if (!workspace || ws_bytes < need)
+    return fail(SQ_ERR_WORKSPACE, "%s: workspace %zu bytes < %zu required", who, ws_bytes, need);
+  if (!aligned(workspace, 16)) return fail(SQ_ERR_ALIGN, "%s: workspace must be 16-byte aligned", who);
+  cudaError_t e = launch_attention_kv4(reinterpret_cast<const __half*>(qkv), B, T, Hq, Hkv, pos0, (double)theta,
+                                       kv4_cache(k_codes, k_params, v_codes, v_params), max_ctx,
+                                       reinterpret_cast<__half*>(out), workspace, (cudaStream_t)stream);
+  if (e != cudaSuccess) return cuda_fail(e, who);
+  return SQ_OK;
+}
+
+sq_status sq_logprobs(const void* z, int64_t R, int64_t V, float temperature, const int32_t* tokens,
+                      float* logprob, float* entropy, int top, int32_t* top_tokens, float* top_logprobs,
+                      sq_stream_t stream) {
+  SQ_RANGE();
+  const char* who = "sq_logprobs";
+  if (R < 0 || R > ((int64_t)1 << 24) || V < 1 || V >= ((int64_t)1 << 20))
+    return fail(SQ_ERR_SHAPE, "%s: need 0 <= R <= 2^24, 1 <= V < 2^20 (R=%lld V=%lld)", who, (long long)R,
+                (long long)V);
+  if (top < 0 || top > kLogprobsMaxTop || top > V)
+    return fail(SQ_ERR_SHAPE, "%s: need 0 <= top <= %d and top <= V (top=%d)", who, kLogprobsMaxTop, top);
+  if (!(temperature > 0.0f) || !std::isfinite(temperature) || !std::isfinite(1.0f / temperature))
+    return fail(SQ_ERR_INVALID_ARG, "%s: temperature must be positive and finite, and so its reciprocal", who);
+  if (R == 0) return SQ_OK;
+  if (!z) return fail(SQ_ERR_INVALID_ARG, "%s: NULL z", who);
+  if ((tokens == nullptr) != (logprob == nullptr))
+    return fail(SQ_ERR_INVALID_ARG, "%s: tokens and logprob go together", who);
+  if (top > 0 && (!top_tokens || !top_logprobs))
+    return fail(SQ_ERR_INVALID_ARG, "%s: NULL top_tokens or top_logprobs", who);
+  if (!logprob && !entropy && top == 0) return fail(SQ_ERR_INVALID_ARG, "%s: nothing is asked for", who);
+  if (!aligned(z, 2) || !aligned(tokens, 4) || !aligned(logprob, 4) || !aligned(entropy, 4) ||
+      !aligned(top_tokens, 4) || !aligned(top_logprobs, 4))
+    return fail(SQ_ERR_ALIGN, "%s: z must be 2-byte, other pointers 4-byte aligned", who);
+  const LogprobArgs a = {reinterpret_cast<const __half*>(z), tokens, logprob, entropy, top_tokens, top_logprobs,
+                         R, V, top, 1.0f / temperature};
+  cudaError_t e = launch_logprobs(a, (cudaStream_t)stream);
+  if (e != cudaSuccess) return cuda_fail(e, who);
   return SQ_OK;
 }
 

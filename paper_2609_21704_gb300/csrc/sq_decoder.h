@@ -4,6 +4,7 @@
 #pragma once
 
 #include "sq_internal.h"
+#include "sq_rope.h"
 
 namespace sq {
 
@@ -28,6 +29,7 @@ cudaError_t launch_spec_commit(const int32_t* n, const int32_t* tokens, int ldt,
                                int cap, int32_t* len, int32_t* pos, int32_t* last2, cudaStream_t st);
 cudaError_t launch_spec_drafts(const int32_t* samples, const int32_t* last2, int B, int K, int32_t* verify,
                                int32_t* draft, cudaStream_t st);
+RopeFreq rope_freq(double theta);  // the table of one theta (host)
 cudaError_t take_attn_status(uint32_t* bits);
 
 }  // namespace sq
