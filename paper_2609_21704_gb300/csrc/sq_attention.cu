@@ -29,9 +29,7 @@ __device__ unsigned int g_attn_status;
 constexpr int kAttnWarps = 4;
 constexpr int kAttnThreads = 32 * kAttnWarps;
 constexpr int kMaxT = 32;           // new tokens per sequence and call
-// Per-query partial record in the workspace: (max, sum, 2 unused, o[D]):
-// 132 floats = 528 bytes, so records and their o[] stay 16-byte aligned.
-constexpr int kPartStride = kHeadDim + 4;
+constexpr int kPartStride = kAttnPartStride;
 constexpr int kPartO = 4;
 
 // ---- RMSNorm -----------------------------------------------------------------
@@ -976,6 +974,22 @@ cudaError_t launch_attention(const __half* qkv, int B, int T, int Hq, int Hkv, c
   if (a.Q <= 16) return launch_attn_inst<1, 2>(a, st);
   if (a.Q <= 32) return launch_attn_inst<2, 2>(a, st);
   return launch_attn_inst<4, 2>(a, st);
+}
+
+cudaError_t launch_attention_combine(float* part, int B, int T, int Hq, int Hkv, int nsplit, __half* out,
+                                     cudaStream_t st) {
+  AttnArgs a = {};
+  a.part = part;
+  a.out = out;
+  a.B = B;
+  a.T = T;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.G = Hq / Hkv;
+  a.Q = a.G * T;
+  a.nsplit = nsplit;
+  return launch_pdl(attention_combine_kernel, dim3((unsigned)(B * Hkv), (unsigned)a.Q), dim3(kHeadDim),
+                    (size_t)2 * nsplit * sizeof(float), st, a);
 }
 
 cudaError_t launch_kv_rollback(const int32_t* base, const int32_t* n, int B, int limit, int32_t* len,

@@ -29,6 +29,12 @@ cudaError_t launch_spec_commit(const int32_t* n, const int32_t* tokens, int ldt,
                                int cap, int32_t* len, int32_t* pos, int32_t* last2, cudaStream_t st);
 cudaError_t launch_spec_drafts(const int32_t* samples, const int32_t* last2, int B, int K, int32_t* verify,
                                int32_t* draft, cudaStream_t st);
+// Per-query partial record of decode attention: (max, sum, 2 unused, o[D]):
+// 132 floats = 528 bytes, so records and their o[] stay 16-byte aligned.
+constexpr int kAttnPartStride = kHeadDim + 4;
+// out from the records part [(B Hkv) nsplit Q kAttnPartStride] of nsplit shares of the keys
+cudaError_t launch_attention_combine(float* part, int B, int T, int Hq, int Hkv, int nsplit, __half* out,
+                                     cudaStream_t st);
 RopeFreq rope_freq(double theta);  // the table of one theta (host)
 cudaError_t take_attn_status(uint32_t* bits);
 

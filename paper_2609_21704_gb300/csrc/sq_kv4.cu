@@ -14,11 +14,15 @@
 // dimensions) of the even position, then those of the odd one.
 #include "sq_packed.cuh"
 
+#include <mutex>
+
 namespace sq {
 
 static __device__ unsigned int g_kv4_status;
 
 // Codes of one row whose lane holds the fp16 values x[4]; par: scale and lowest.
+// A quotient comes from the reciprocal (within 2^-19 of the quotient: it is at
+// most 15); only where that leaves the rounding open is it divided.
 __device__ __forceinline__ uint32_t kv4_encode(const float x[4], uint32_t& par, bool& fine) {
   float lo = fminf(fminf(x[0], x[1]), fminf(x[2], x[3]));
   float hi = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
@@ -38,51 +42,64 @@ __device__ __forceinline__ uint32_t kv4_encode(const float x[4], uint32_t& par, 
   const float s = __half2float(s16);
   par = (uint32_t)__half_as_ushort(s16) | ((uint32_t)__half_as_ushort(__float2half_rn(lo)) << 16);
   if (s == 0.0f) return 0;
+  const float inv = __frcp_rn(s);
   uint32_t w = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const float c = rintf(__fdiv_rn(__fsub_rn(x[e], lo), s));
+    const float d = __fsub_rn(x[e], lo);
+    const float q = d * inv;
+    float c = rintf(q);
+    if (fabsf(fabsf(q - c) - 0.5f) < 1e-5f) c = rintf(__fdiv_rn(d, s));
     w |= (uint32_t)fminf(fmaxf(c, 0.0f), 15.0f) << (4 * e);
   }
   return w;
 }
 
-// One CTA per row, a warp per (key/value head, key or value).
-__global__ void __launch_bounds__(128) kv4_append_kernel(const __half* __restrict__ qkv, const Packed pk, int Hq,
-                                                         int Hkv, const RopeFreq rf, const KV4Cache c) {
+// One CTA per kAppendRows rows (their rotation tables are shared by all heads),
+// a warp per (row, key/value head, key or value); a warp reads 256 contiguous
+// bytes, and the table's two entries of a lane lie together.
+constexpr int kAppendRows = 4, kAppendThreads = 256;
+__global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(const __half* __restrict__ qkv, const Packed pk,
+                                                                    int Hq, int Hkv, const RopeFreq rf,
+                                                                    const KV4Cache c) {
   griddep_wait();
   griddep_launch_dependents();
-  __shared__ RopeCS cs[kHeadDim / 2];
-  const int64_t row = blockIdx.x;
-  const PackedRow pr = packed_row(pk, row);
-  if (threadIdx.x == 0 && (pr.bad || (pr.b >= 0 && !pr.ok))) atomicOr(&g_kv4_status, SQ_DEV_BAD_POSITION);
-  if (pr.b < 0 || !pr.ok) return;
-  if (threadIdx.x < kHeadDim / 2) cs[threadIdx.x] = rope_cs_pair(pr.pos, rf.f[threadIdx.x]);
+  __shared__ RopeCS cs[kAppendRows][kHeadDim / 2];
+  __shared__ int seq[kAppendRows], pos[kAppendRows];
+  const int64_t row0 = (int64_t)blockIdx.x * kAppendRows;
+  const int tid = threadIdx.x, lane = tid & 31;
+  if (packed_rows<kAppendRows>(pk, row0, seq, pos, &g_kv4_status)) return;
+  {
+    const int i = tid / (kHeadDim / 2), d = tid % (kHeadDim / 2);
+    if (seq[i] >= 0 && pos[i] >= 0) cs[i][d] = rope_cs_pair(pos[i], rf.f[d]);
+  }
   __syncthreads();
-  const int lane = threadIdx.x & 31;
-  const __half* xr = qkv + row * (int64_t)(Hq + 2 * Hkv) * kHeadDim;
-  for (int i = threadIdx.x >> 5; i < 2 * Hkv; i += blockDim.x >> 5) {
+  for (int j = tid >> 5; j < kAppendRows * 2 * Hkv; j += kAppendThreads >> 5) {
+    const int r = j / (2 * Hkv), i = j - r * 2 * Hkv;
+    if (seq[r] < 0 || pos[r] < 0) continue;
     const bool val = i >= Hkv;
     const int h = val ? i - Hkv : i;
-    const int64_t slot = ((int64_t)pr.b * Hkv + h) * pk.max_ctx + pr.pos;
-    const __half* src = xr + (int64_t)(Hq + i) * kHeadDim;
+    const int64_t slot = ((int64_t)seq[r] * Hkv + h) * pk.max_ctx + pos[r];
+    const __half* src = qkv + ((row0 + r) * (int64_t)(Hq + 2 * Hkv) + Hq + i) * kHeadDim;
     float x[4];
     bool fine;
     uint32_t par, w;
     if (val) {  // dimensions 4 lane ..
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = __half2float(src[4 * lane + e]);
+      const uint2 v = reinterpret_cast<const uint2*>(src)[lane];
+      const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&v.x));
+      const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&v.y));
+      x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
       w = kv4_encode(x, par, fine);
       uint16_t* dst = reinterpret_cast<uint16_t*>(c.vc + (slot >> 1) * kHeadDim);
       dst[2 * lane + (slot & 1)] = (uint16_t)w;
     } else {  // dimensions 2 lane, 2 lane + 1 and 64 more
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const RopeCS r = cs[2 * lane + e];
-        const float a = __half2float(src[2 * lane + e]), b = __half2float(src[2 * lane + e + kHeadDim / 2]);
-        x[e] = __half2float(__float2half_rn(rope_dot(a, r.c, -b, r.s)));
-        x[e + 2] = __half2float(__float2half_rn(rope_dot(b, r.c, a, r.s)));
-      }
+      const float2 a = __half22float2(reinterpret_cast<const __half2*>(src)[lane]);
+      const float2 b = __half22float2(reinterpret_cast<const __half2*>(src)[lane + 32]);
+      const RopeCS r0 = cs[r][2 * lane], r1 = cs[r][2 * lane + 1];
+      x[0] = __half2float(__float2half_rn(rope_dot(a.x, r0.c, -b.x, r0.s)));
+      x[1] = __half2float(__float2half_rn(rope_dot(a.y, r1.c, -b.y, r1.s)));
+      x[2] = __half2float(__float2half_rn(rope_dot(b.x, r0.c, a.x, r0.s)));
+      x[3] = __half2float(__float2half_rn(rope_dot(b.y, r1.c, a.y, r1.s)));
       w = kv4_encode(x, par, fine);
       c.kc[slot * (kHeadDim / 2) + lane] = (uint8_t)w;
       c.kc[slot * (kHeadDim / 2) + lane + 32] = (uint8_t)(w >> 8);
@@ -96,110 +113,577 @@ __global__ void __launch_bounds__(128) kv4_append_kernel(const __half* __restric
 
 cudaError_t launch_kv4_append(const __half* qkv, const Packed& pk, int Hq, int Hkv, double theta,
                               const KV4Cache& c, cudaStream_t st) {
-  return launch_pdl(kv4_append_kernel, dim3((unsigned)pk.N), dim3(128), 0, st, qkv, pk, Hq, Hkv,
-                    rope_freq(theta), c);
+  return launch_pdl(kv4_append_kernel, dim3((unsigned)((pk.N + kAppendRows - 1) / kAppendRows)), dim3(kAppendThreads), 0,
+                    st, qkv, pk, Hq, Hkv, rope_freq(theta), c);
 }
 
 __device__ __forceinline__ float2 kv4_params(const __half* p, int64_t slot) {
   return __half22float2(reinterpret_cast<const __half2*>(p)[slot]);
 }
 
-// One CTA per 64 positions of a (sequence, head), a warp per row.
+// One CTA per 64 positions of a (sequence, head); a thread two neighbouring
+// positions' 16 dimensions of keys and values: 8-byte loads, 16-byte stores.
 constexpr int kUnpackRows = 64;
-__global__ void __launch_bounds__(128) kv4_unpack_kernel(const KV4Cache c, int Hkv, int64_t max_ctx,
+__device__ __forceinline__ uint32_t kv4_half2(uint32_t nibbles, float2 p) {
+  const __half2 r = __floats2half2_rn(fmaf((float)(nibbles & 15), p.x, p.y), fmaf((float)((nibbles >> 4) & 15), p.x, p.y));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// Eight dimensions from four bytes.
+__device__ __forceinline__ uint4 kv4_half8(uint32_t w, float2 p) {
+  return make_uint4(kv4_half2(w, p), kv4_half2(w >> 8, p), kv4_half2(w >> 16, p), kv4_half2(w >> 24, p));
+}
+__global__ void __launch_bounds__(256) kv4_unpack_kernel(const KV4Cache c, int Hkv, int64_t max_ctx,
                                                          const int32_t* __restrict__ first,
                                                          const int32_t* __restrict__ last, __half* __restrict__ k,
                                                          __half* __restrict__ v) {
   griddep_wait();
   griddep_launch_dependents();
-  const int b = blockIdx.z, h = blockIdx.y, lane = threadIdx.x & 31;
+  const int b = blockIdx.z, h = blockIdx.y;
   const int64_t lo = first[b], hi = last[b];
   if (lo >= hi) return;
   if (lo < 0 || hi > max_ctx) {
     if (threadIdx.x == 0 && blockIdx.x == 0) atomicOr(&g_kv4_status, SQ_DEV_BAD_POSITION);
     return;
   }
-  const int64_t j0 = (int64_t)blockIdx.x * kUnpackRows;
-  for (int i = threadIdx.x >> 5; i < kUnpackRows; i += blockDim.x >> 5) {
-    const int64_t j = j0 + i;
-    if (j < lo || j >= hi) continue;
-    const int64_t slot = ((int64_t)b * Hkv + h) * max_ctx + j;
-    const float2 kp = kv4_params(c.kp, slot), vp = kv4_params(c.vp, slot);
-    const uint32_t kw = reinterpret_cast<const uint16_t*>(c.kc + slot * (kHeadDim / 2))[lane];
-    const uint32_t vw = reinterpret_cast<const uint16_t*>(c.vc + (slot >> 1) * kHeadDim)[2 * lane + (slot & 1)];
-    __half* kd = k + slot * kHeadDim + 4 * lane;
-    __half* vd = v + slot * kHeadDim + 4 * lane;
+  const int64_t j = (int64_t)blockIdx.x * kUnpackRows + (threadIdx.x >> 3) * 2;
+  const int u = threadIdx.x & 7;  // dimensions 16 u ..
+  if (j + 1 < lo || j >= hi) return;
+  const int64_t slot = ((int64_t)b * Hkv + h) * max_ctx + j;
+  const uint4 vw = reinterpret_cast<const uint4*>(c.vc + (slot >> 1) * kHeadDim)[u];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      kd[e] = __float2half_rn(fmaf((float)((kw >> (4 * e)) & 15), kp.x, kp.y));
-      vd[e] = __float2half_rn(fmaf((float)((vw >> (4 * e)) & 15), vp.x, vp.y));
-    }
+  for (int e = 0; e < 2; ++e) {
+    if (j + e < lo || j + e >= hi) continue;
+    const float2 kp = kv4_params(c.kp, slot + e), vp = kv4_params(c.vp, slot + e);
+    const uint2 kw = reinterpret_cast<const uint2*>(c.kc + (slot + e) * (kHeadDim / 2))[u];
+    uint4* kd = reinterpret_cast<uint4*>(k + (slot + e) * kHeadDim) + 2 * u;
+    uint4* vd = reinterpret_cast<uint4*>(v + (slot + e) * kHeadDim) + 2 * u;
+    const uint32_t sel = e ? 0x7632u : 0x5410u;  // the position's two bytes of every four
+    kd[0] = kv4_half8(kw.x, kp);
+    kd[1] = kv4_half8(kw.y, kp);
+    vd[0] = kv4_half8(__byte_perm(vw.x, vw.y, sel), vp);
+    vd[1] = kv4_half8(__byte_perm(vw.z, vw.w, sel), vp);
   }
 }
 
 cudaError_t launch_kv4_unpack(const KV4Cache& c, int B, int Hkv, int64_t max_ctx, const int32_t* first,
                               const int32_t* last, __half* k, __half* v, cudaStream_t st) {
   const dim3 grid((unsigned)((max_ctx + kUnpackRows - 1) / kUnpackRows), (unsigned)Hkv, (unsigned)B);
-  return launch_pdl(kv4_unpack_kernel, grid, dim3(128), 0, st, c, Hkv, max_ctx, first, last, k, v);
+  return launch_pdl(kv4_unpack_kernel, grid, dim3(256), 0, st, c, Hkv, max_ctx, first, last, k, v);
 }
 
-// One CTA per new token, a warp per query head; a lane holds dimensions 4 lane ..
-__global__ void __launch_bounds__(128) attention_kv4_simple_kernel(const __half* __restrict__ qkv, int T, int Hq,
-                                                                   int Hkv, const int32_t* __restrict__ pos0,
-                                                                   const RopeFreq rf, const KV4Cache c,
-                                                                   int64_t max_ctx, __half* __restrict__ out) {
+// ---- attention over the cache ----------------------------------------------------
+
+struct KV4AttnArgs {
+  const __half* qkv;
+  KV4Cache c;
+  const int32_t* pos0;
+  __half* out;
+  float* part;  // [(B Hkv) nsplit Q kAttnPartStride] where the shares meet in a second launch
+  int B, T, Hq, Hkv, G, Q;
+  int64_t max_ctx;
+  int nsplit;   // CTAs sharing the keys of a (sequence, key/value head, eight queries)
+  int cluster;  // they form a cluster and meet in shared memory
+  RopeFreq rf;
+};
+
+constexpr int kK4Warps = 4, kK4Threads = 32 * kK4Warps;
+constexpr int kK4Keys = 16;                   // keys of a warp's step
+constexpr int kK4Stages = 4;                  // steps in flight a warp
+constexpr int kK4Codes = kK4Keys * 64;        // bytes of a step's key (value) codes
+constexpr int kK4Stage = 2 * kK4Codes + 2 * kK4Keys * 4;
+constexpr int kK4Rec = kAttnPartStride;       // floats of a query's partial result
+constexpr int kK4OffQ = 0;                    // queries, two fp16 terms: [2][8][128]
+constexpr int kK4OffFac = kK4OffQ + 2 * 8 * kHeadDim * 2;  // their factors and sums
+constexpr int kK4OffRing = kK4OffFac + 64;
+constexpr int kK4OffRec = kK4OffRing;         // the records, over the ring: one a warp, then the CTA's
+constexpr int kK4Smem = kK4OffRing + (kK4Warps * kK4Stages * kK4Stage > (kK4Warps + 1) * 8 * kK4Rec * 4
+                                          ? kK4Warps * kK4Stages * kK4Stage
+                                          : (kK4Warps + 1) * 8 * kK4Rec * 4);
+
+__device__ __forceinline__ void k4_mma(float d[4], const uint32_t a[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
+      "{%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void k4_cp16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+// Eight codes to four pairs holding 64 + n: nibbles e and e + 4 of the word in
+// pair e.  A nibble in bits 4 .. 7 of an fp16 value of exponent 6 counts ones; the
+// 64 is taken off the sums (they stay within 2^-17 of exact: the products are,
+// and fp32 has 13 bits more than the result needs).
+__device__ __forceinline__ void k4_codes(uint32_t w, uint32_t r[4]) {
+  constexpr uint32_t kMask = 0x00f000f0u, kOne = 0x54005400u;
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r[0]) : "r"(w << 4), "r"(kMask), "r"(kOne));
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r[1]) : "r"(w), "r"(kMask), "r"(kOne));
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r[2]) : "r"(w >> 4), "r"(kMask), "r"(kOne));
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r[3]) : "r"(w >> 8), "r"(kMask), "r"(kOne));
+}
+__device__ __forceinline__ float k4_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// x = hi + lo to 22 bits (fp16 terms; a hi that is not finite carries x alone).
+__device__ __forceinline__ void k4_split(float x, __half& hi, __half& lo) {
+  hi = __float2half_rn(x);
+  const float h = __half2float(hi);
+  lo = isfinite(h) ? __float2half_rn(x - h) : __ushort_as_half(0);
+}
+__device__ __forceinline__ uint32_t k4_pack(__half a, __half b) {
+  return (uint32_t)__half_as_ushort(a) | ((uint32_t)__half_as_ushort(b) << 16);
+}
+__device__ __forceinline__ float4 k4_ld_cluster(const float* local, uint32_t rank) {
+  uint32_t r;
+  float4 v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(local)), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(r)
+               : "memory");
+  return v;
+}
+__device__ __forceinline__ void k4_cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// One CTA: eight queries (q = g T + t) of a (sequence, key/value head) against a
+// share of its keys, four warps taking steps of 16 keys in turn.
+//
+// A step's codes are 2 KB that lie as the products want them: a lane copies
+// (cp.async, four steps ahead, no barrier) and reads 16 bytes of a key's row and
+// 16 of two positions' values, and every word of them becomes operands of
+// mma.m16n8k16 in the lane itself: keys as the columns of Q K^T in an order of
+// dimensions that the queries share, values as the columns of P V with positions
+// in pairs, so nothing is moved between lanes or through shared memory.  Scale
+// and lowest value of a row enter beside the products.  Queries and weights are
+// two fp16 terms each (rows 0..7 and 8..15 of a tile): nothing held in 32 bits is
+// rounded to 16.  The running maximum may lag by 2^5 before sums are rescaled, and
+// so may the power of two that brings weights times value scales into fp16's
+// range.  Bound: the codes' bytes at one token of up to eight heads a group (about
+// 230 instructions a step against 370 issue slots in the bytes' time), the products
+// for more queries, which read the same codes again out of L2.
+__global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4AttnArgs a) {
   griddep_wait();
   griddep_launch_dependents();
-  __shared__ RopeCS cs[kHeadDim / 2];
-  const int64_t row = blockIdx.x;
-  const int b = (int)(row / T), t = (int)(row - (int64_t)b * T), lane = threadIdx.x & 31;
-  const int64_t p0 = pos0[b];
-  const bool ok = p0 >= 0 && p0 + T <= max_ctx;
-  if (!ok && threadIdx.x == 0) atomicOr(&g_kv4_status, SQ_DEV_BAD_POSITION);
-  const int pos = ok ? (int)p0 + t : -1;
-  if (threadIdx.x < kHeadDim / 2) cs[threadIdx.x] = rope_cs_pair(pos, rf.f[threadIdx.x]);
+  extern __shared__ __align__(128) uint8_t k4_smem[];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
+  const int bh = (int)(blockIdx.x / (unsigned)a.nsplit), split = (int)(blockIdx.x - (unsigned)bh * a.nsplit);
+  const int b = bh / a.Hkv, kvh = bh - b * a.Hkv, q0 = blockIdx.y * 8, T = a.T;
+  const int64_t p0l = a.pos0[b];
+  const bool valid = p0l >= 0 && p0l + T <= a.max_ctx;
+  if (!valid && split == 0 && blockIdx.y == 0 && tid == 0) atomicOr(&g_kv4_status, SQ_DEV_BAD_POSITION);
+  const int p0 = valid ? (int)p0l : 0, len = valid ? p0 + T : 0;
+  const int steps = (len + kK4Keys - 1) / kK4Keys;
+  const int s0 = (int)((int64_t)split * steps / a.nsplit), s1 = (int)((int64_t)(split + 1) * steps / a.nsplit);
+
+  // this warp's ring; lane pieces of a step: keys 0..7 and 8..15, values likewise
+  const uint32_t ring = smem_u32(k4_smem) + kK4OffRing + warp * (kK4Stages * kK4Stage);
+  const uint8_t* slot0 = k4_smem + kK4OffRing + warp * (kK4Stages * kK4Stage);
+  const int64_t row = (int64_t)bh * a.max_ctx;
+  auto request = [&](int step, int stage) {
+    if (step < s1) {
+      const int64_t key = row + (int64_t)step * kK4Keys;
+      const uint32_t dst = ring + stage * kK4Stage + lane * 16;
+      const uint8_t* ks = a.c.kc + key * 64 + lane * 16;
+      const uint8_t* vs = a.c.vc + key * 64 + t4 * 128 + g * 16;
+      k4_cp16(dst, ks);
+      k4_cp16(dst + 512, ks + 512);
+      k4_cp16(dst + kK4Codes, vs);
+      k4_cp16(dst + kK4Codes + 512, vs + 512);
+      if (lane < 8)  // parameters: 64 bytes of keys, 64 of values
+        k4_cp16(ring + stage * kK4Stage + 2 * kK4Codes + lane * 16,
+                reinterpret_cast<const uint8_t*>((lane < 4 ? a.c.kp : a.c.vp) + key * 2) + (lane & 3) * 16);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  int step = s0 + warp;
+#pragma unroll
+  for (int i = 0; i < kK4Stages - 1; ++i) request(step + i * kK4Warps, i);
+
+  // the queries: a warp takes two, rotated in fp32, scaled by a power of two
+  __half* qs = reinterpret_cast<__half*>(k4_smem + kK4OffQ);
+  float* fac = reinterpret_cast<float*>(k4_smem + kK4OffFac);
+  if (s0 < s1)
+    for (int i = warp; i < 8; i += kK4Warps) {
+      const int q = q0 + i;
+      float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // d = lane, lane + 32, lane + 64, lane + 96
+      if (q < a.Q) {
+        const int hg = q / T, t = q - hg * T;
+        const __half* x = a.qkv + (((int64_t)b * T + t) * (a.Hq + 2 * a.Hkv) + kvh * a.G + hg) * kHeadDim + lane;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const RopeCS r = rope_cs_pair(p0 + t, a.rf.f[lane + 32 * e]);
+          const float x1 = __half2float(x[32 * e]), x2 = __half2float(x[32 * e + 64]);
+          v[e] = x1 * r.c.h - x2 * r.s.h;
+          v[e + 2] = x2 * r.c.h + x1 * r.s.h;
+        }
+      }
+      const float am = warp_max(fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3]))));
+      int ex = 10;
+      if (am > 0.0f && isfinite(am)) ex = max((int)(__float_as_uint(am) >> 23) - 127, -100);
+      const float up = __uint_as_float((uint32_t)(127 + 10 - ex) << 23);  // largest value to [2^10, 2^11)
+      float sum = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        __half hi, lo;
+        k4_split(v[e] * up, hi, lo);
+        qs[i * kHeadDim + lane + 32 * e] = hi;
+        qs[(8 + i) * kHeadDim + lane + 32 * e] = lo;
+        sum += __half2float(hi) + __half2float(lo);
+      }
+      sum = warp_sum(sum);
+      if (lane == 0) {
+        // scores in units of log 2
+        fac[i] = 0.08838834764831845f * 1.4426950408889634f * __uint_as_float((uint32_t)(127 + ex - 10) << 23);
+        fac[8 + i] = sum;
+      }
+    }
   __syncthreads();
-  const int G = Hq / Hkv;
-  for (int h = threadIdx.x >> 5; h < Hq; h += blockDim.x >> 5) {
-    const __half* x = qkv + row * (int64_t)(Hq + 2 * Hkv) * kHeadDim + (int64_t)h * kHeadDim;
-    float q[4];
+  uint32_t qa[8][4];
+  float fq = 0.0f, qsum = 0.0f;
+  if (s0 < s1) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int d = 4 * lane + e, d1 = d % (kHeadDim / 2);
-      const float x1 = __half2float(x[d1]), x2 = __half2float(x[d1 + kHeadDim / 2]);
-      const RopeCS r = cs[d1];
-      q[e] = d < kHeadDim / 2 ? x1 * r.c.h - x2 * r.s.h : x2 * r.c.h + x1 * r.s.h;
-    }
-    float m = -INFINITY, l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int j = 0; j <= pos; ++j) {
-      const int64_t slot = ((int64_t)b * Hkv + h / G) * max_ctx + j;
-      const float2 kp = kv4_params(c.kp, slot), vp = kv4_params(c.vp, slot);
-      const uint32_t kw = reinterpret_cast<const uint16_t*>(c.kc + slot * (kHeadDim / 2))[lane];
-      const uint32_t vw = reinterpret_cast<const uint16_t*>(c.vc + (slot >> 1) * kHeadDim)[2 * lane + (slot & 1)];
-      float s = 0.0f;
+    for (int kk = 0; kk < 8; ++kk)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s = fmaf(q[e], fmaf((float)((kw >> (4 * e)) & 15), kp.x, kp.y), s);
-      s = warp_sum(s) * 0.08838834764831845f;
-      const float mn = fmaxf(m, s);
-      const float f = m == -INFINITY ? 0.0f : expf(m - mn), p = expf(s - mn);
-      m = mn;
-      l = l * f + p;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = o[e] * f + p * fmaf((float)((vw >> (4 * e)) & 15), vp.x, vp.y);
-    }
-    __half* dst = out + row * (int64_t)Hq * kHeadDim + (int64_t)h * kHeadDim + 4 * lane;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) dst[e] = __float2half_rn(l == 0.0f ? 0.0f : o[e] / l);
+      for (int half = 0; half < 2; ++half) {
+        const int i = 2 * kk + half, d = 32 * t4 + 8 * (i >> 2) + (i & 3);
+        qa[kk][2 * half] = k4_pack(qs[g * kHeadDim + d], qs[g * kHeadDim + d + 4]);
+        qa[kk][2 * half + 1] = k4_pack(qs[(8 + g) * kHeadDim + d], qs[(8 + g) * kHeadDim + d + 4]);
+      }
+    fq = fac[g];
+    qsum = fac[8 + g];
   }
+  const int lim = p0 + (q0 + g) % T;  // the last position this lane's query sees
+
+  float o[16][4], m = -INFINITY, l = 0.0f, zl = 0.0f, zw = 0.0f;
+  float vcap = 0.0f, vup = 1.0f;  // value scales up to vcap; vup brings them to 2^9
+#pragma unroll
+  for (int i = 0; i < 16; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
+
+  for (int it = 0; step < s1; ++it, step += kK4Warps) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kK4Stages - 2) : "memory");
+    __syncwarp();  // the parameters are other lanes' copies
+    const uint8_t* sl = slot0 + (it % kK4Stages) * kK4Stage;
+    float sc[2][2], ws[2][2], wl[2][2];
+    const bool edge = (step + 1) * kK4Keys > p0 + 1;
+    float mx = -INFINITY, vm = 0.0f;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const uint4 kw = *reinterpret_cast<const uint4*>(sl + n * 512 + lane * 16);
+      const uint32_t w[4] = {kw.x, kw.y, kw.z, kw.w};
+      float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t r[4];
+        k4_codes(w[i], r);
+        k4_mma(s, qa[2 * i], r[0], r[1]);
+        k4_mma(s, qa[2 * i + 1], r[2], r[3]);
+      }
+      const uint2 kp = *reinterpret_cast<const uint2*>(sl + 2 * kK4Codes + n * 32 + t4 * 8);
+      const uint2 vp = *reinterpret_cast<const uint2*>(sl + 2 * kK4Codes + 64 + n * 32 + t4 * 8);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float2 k2 = __half22float2(*reinterpret_cast<const __half2*>(e ? &kp.y : &kp.x));
+        const float2 v2 = __half22float2(*reinterpret_cast<const __half2*>(e ? &vp.y : &vp.x));
+        sc[n][e] = fq * fmaf(k2.x, s[e] + s[e + 2], fmaf(-64.0f, k2.x, k2.y) * qsum);
+        ws[n][e] = v2.x;
+        wl[n][e] = v2.y;
+        if (edge && step * kK4Keys + 8 * n + 2 * t4 + e > lim) {
+          sc[n][e] = -INFINITY;
+          ws[n][e] = wl[n][e] = 0.0f;
+        }
+        mx = fmaxf(mx, sc[n][e]);
+        vm = fmaxf(vm, ws[n][e]);
+      }
+    }
+    if (__any_sync(0xffffffffu, mx - m > 5.0f || vm > vcap)) {
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+      vm = warp_max(vm);
+      const float mn = fmaxf(m, mx);
+      float f = m == -INFINITY ? 0.0f : k4_ex2(m - mn), fv = 1.0f;
+      m = mn;
+      if (vm > vcap) {
+        // the power of two above vm becomes 1/32: weights up to 2^5 stay below 2^15
+        const float cap = __uint_as_float(((__float_as_uint(vm) >> 23) + 1) << 23);
+        const float up = 512.0f / cap;
+        fv = up / vup;
+        vcap = cap;
+        vup = up;
+      }
+      l *= f;
+      zl *= f;
+      f *= fv;
+      zw *= f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[i][e] *= f;
+    }
+    const float mm = m == -INFINITY ? 0.0f : m;
+    uint32_t pa[4];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      __half hi[2], lo[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float p = k4_ex2(sc[n][e] - mm);
+        l += p;
+        zl = fmaf(p, wl[n][e], zl);
+        const float x = p * (ws[n][e] * vup);
+        k4_split(x, hi[e], lo[e]);
+        zw += x;
+      }
+      pa[2 * n] = k4_pack(hi[0], hi[1]);
+      pa[2 * n + 1] = k4_pack(lo[0], lo[1]);
+    }
+    const uint4 va = *reinterpret_cast<const uint4*>(sl + kK4Codes + lane * 16);
+    const uint4 vb = *reinterpret_cast<const uint4*>(sl + kK4Codes + 512 + lane * 16);
+    const uint32_t wa[4] = {va.x, va.y, va.z, va.w}, wb[4] = {vb.x, vb.y, vb.z, vb.w};
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      uint32_t ra[4], rb[4];
+      k4_codes(wa[u], ra);
+      k4_codes(wb[u], rb);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) k4_mma(o[4 * u + e], pa, ra[e], rb[e]);
+    }
+    __syncwarp();  // every lane has read the parameters
+    request(step + (kK4Stages - 1) * kK4Warps, (it + kK4Stages - 1) % kK4Stages);
+  }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  __syncthreads();
+
+  // ---- records (m, l, -, -, o[D]) over the ring: a warp's, then the CTA's
+  float* rec = reinterpret_cast<float*>(k4_smem + kK4OffRec);
+  {
+#pragma unroll
+    for (int i = 1; i < 4; i <<= 1) {
+      l += __shfl_xor_sync(0xffffffffu, l, i);
+      zl += __shfl_xor_sync(0xffffffffu, zl, i);
+      zw += __shfl_xor_sync(0xffffffffu, zw, i);
+    }
+    float* r = rec + (warp * 8 + g) * kK4Rec;
+    if (t4 == 0) {
+      r[0] = m * 0.6931471805599453f;  // (natural units, as attention_combine_kernel has them)
+      r[1] = l;
+    }
+    const float down = 1.0f / vup;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float4 x;
+        x.x = fmaf(o[4 * u][e] + o[4 * u][e + 2] - 64.0f * zw, down, zl);
+        x.y = fmaf(o[4 * u + 1][e] + o[4 * u + 1][e + 2] - 64.0f * zw, down, zl);
+        x.z = fmaf(o[4 * u + 2][e] + o[4 * u + 2][e + 2] - 64.0f * zw, down, zl);
+        x.w = fmaf(o[4 * u + 3][e] + o[4 * u + 3][e + 2] - 64.0f * zw, down, zl);
+        *reinterpret_cast<float4*>(r + 4 + 16 * (2 * t4 + e) + 4 * u) = x;
+      }
+  }
+  __syncthreads();
+  const int nq = min(8, a.Q - q0);
+  float* mine = rec + kK4Warps * 8 * kK4Rec;
+  for (int i = tid; i < nq * (kHeadDim / 4); i += kK4Threads) {
+    const int q = i / (kHeadDim / 4), d4 = i % (kHeadDim / 4);
+    float M = -INFINITY, L = 0.0f;
+    float4 O = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int w = 0; w < kK4Warps; ++w) M = fmaxf(M, rec[(w * 8 + q) * kK4Rec]);
+#pragma unroll
+    for (int w = 0; w < kK4Warps; ++w) {
+      const float* r = rec + (w * 8 + q) * kK4Rec;
+      if (r[0] == -INFINITY) continue;
+      const float f = expf(r[0] - M);
+      const float4 v = *reinterpret_cast<const float4*>(r + 4 + 4 * d4);
+      L = fmaf(f, r[1], L);
+      O.x = fmaf(f, v.x, O.x);
+      O.y = fmaf(f, v.y, O.y);
+      O.z = fmaf(f, v.z, O.z);
+      O.w = fmaf(f, v.w, O.w);
+    }
+    float* r = mine + q * kK4Rec;
+    if (d4 == 0) {
+      r[0] = M;
+      r[1] = L;
+    }
+    *reinterpret_cast<float4*>(r + 4 + 4 * d4) = O;
+  }
+  __syncthreads();
+
+  if (!a.cluster && a.nsplit > 1) {  // to the workspace, merged by attention_combine_kernel
+    float* part = a.part + (((int64_t)bh * a.nsplit + split) * a.Q + q0) * kK4Rec;
+    for (int i = tid; i < nq * (kK4Rec / 4); i += kK4Threads)
+      reinterpret_cast<float4*>(part)[i] = reinterpret_cast<const float4*>(mine)[i];
+    return;
+  }
+  // ---- the cluster's records in rank order; rank r writes its share
+  const int S = a.nsplit;
+  if (S > 1) k4_cluster_sync();
+  const int n = nq * (kHeadDim / 4);
+  const int i0 = (int)((int64_t)split * n / S), i1 = (int)((int64_t)(split + 1) * n / S);
+  for (int i = i0 + tid; i < i1; i += kK4Threads) {
+    const int q = i / (kHeadDim / 4), d4 = i % (kHeadDim / 4);
+    float M = -INFINITY, L = 0.0f;
+    float4 O = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int r0 = 0; r0 < S; r0 += 8) {
+      float4 ml[8], ov[8];  // eight ranks' records in flight
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (r0 + u < S) {
+          ml[u] = k4_ld_cluster(mine + q * kK4Rec, (uint32_t)(r0 + u));
+          ov[u] = k4_ld_cluster(mine + q * kK4Rec + 4 + 4 * d4, (uint32_t)(r0 + u));
+        }
+      float Mn = M;
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (r0 + u < S) Mn = fmaxf(Mn, ml[u].x);
+      if (Mn == -INFINITY) continue;
+      const float f0 = M == -INFINITY ? 0.0f : expf(M - Mn);
+      L *= f0;
+      O.x *= f0; O.y *= f0; O.z *= f0; O.w *= f0;
+      M = Mn;
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (r0 + u < S && ml[u].x != -INFINITY) {
+          const float f = expf(ml[u].x - M);
+          L = fmaf(f, ml[u].y, L);
+          O.x = fmaf(f, ov[u].x, O.x);
+          O.y = fmaf(f, ov[u].y, O.y);
+          O.z = fmaf(f, ov[u].z, O.z);
+          O.w = fmaf(f, ov[u].w, O.w);
+        }
+    }
+    const int qq = q0 + q, hg = qq / T, t = qq - hg * T;
+    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+    __half* dst = a.out + (((int64_t)b * T + t) * a.Hq + kvh * a.G + hg) * kHeadDim + 4 * d4;
+    *reinterpret_cast<uint2*>(dst) =
+        make_uint2(k4_pack(__float2half_rn(O.x * inv), __float2half_rn(O.y * inv)),
+                   k4_pack(__float2half_rn(O.z * inv), __float2half_rn(O.w * inv)));
+  }
+  if (S > 1) k4_cluster_sync();  // no CTA leaves while another reads its records
 }
 
-size_t attention_kv4_workspace_bytes(int B, int T, int Hq, int Hkv, int64_t max_ctx) { return 16; }
+constexpr int kK4MaxCluster = 16;
+constexpr int kK4PerSm = 3;
 
+// How many clusters of S CTAs are resident at once (cached per device).
+static cudaError_t k4_resident(int S, int* n) {
+  static std::mutex mu;
+  static bool ready[64] = {false};
+  static int cache[64][kK4MaxCluster + 1] = {};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  std::lock_guard<std::mutex> lock(mu);
+  if (!ready[dev]) {
+    e = cudaFuncSetAttribute(attention_kv4_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kK4Smem);
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(attention_kv4_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+    ready[dev] = true;
+  }
+  if (cache[dev][S] == 0) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)S);
+    cfg.blockDim = dim3(kK4Threads);
+    cfg.dynamicSmemBytes = kK4Smem;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)S;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    int c = 0;
+    if (cudaOccupancyMaxActiveClusters(&c, attention_kv4_kernel, &cfg) != cudaSuccess) {
+      (void)cudaGetLastError();
+      c = 0;
+    }
+    cache[dev][S] = c + 1;
+  }
+  *n = cache[dev][S] - 1;
+  return cudaSuccess;
+}
+
+// CTAs that share the keys of eight queries: as many as fill the SMs, at least
+// a step of 16 keys for each of a CTA's warps.
+static int64_t k4_shares(int64_t groups, int64_t max_ctx) {
+  const int64_t steps = (max_ctx + kK4Keys - 1) / kK4Keys;
+  int64_t S = kK4PerSm * (int64_t)device_sm_count() / groups;
+  if (S > (steps + kK4Warps - 1) / kK4Warps) S = (steps + kK4Warps - 1) / kK4Warps;
+  return S < 1 ? 1 : S;
+}
+
+size_t attention_kv4_workspace_bytes(int B, int T, int Hq, int Hkv, int64_t max_ctx) {
+  const int64_t Q = (int64_t)(Hq / Hkv) * T, groups = (int64_t)B * Hkv * ((Q + 7) / 8);
+  const int64_t S = groups ? k4_shares(groups, max_ctx) : 1;
+  return (S > 1 ? (size_t)(B * (int64_t)Hkv * S * Q) * kK4Rec * sizeof(float) : 0) + 16;
+}
+
+// Up to 16 shares meet in a cluster (one launch) as long as all clusters are
+// resident; a long cache under few heads takes more, which meet through the
+// workspace and a second launch, from 16 steps a warp on.
 cudaError_t launch_attention_kv4(const __half* qkv, int B, int T, int Hq, int Hkv, const int32_t* pos0,
                                  double theta, const KV4Cache& c, int64_t max_ctx, __half* out, void* ws,
                                  cudaStream_t st) {
-  return launch_pdl(attention_kv4_simple_kernel, dim3((unsigned)(B * T)), dim3(128), 0, st, qkv, T, Hq, Hkv, pos0,
-                    rope_freq(theta), c, max_ctx, out);
+  KV4AttnArgs a = {};
+  a.qkv = qkv;
+  a.c = c;
+  a.pos0 = pos0;
+  a.out = out;
+  a.part = reinterpret_cast<float*>(ws);
+  a.B = B;
+  a.T = T;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.G = Hq / Hkv;
+  a.Q = a.G * T;
+  a.max_ctx = max_ctx;
+  a.rf = rope_freq(theta);
+  const int Z = (a.Q + 7) / 8;
+  const int64_t groups = (int64_t)B * Hkv * Z;
+  int64_t S = k4_shares(groups, max_ctx);
+  a.cluster = S > 1 && (S <= kK4MaxCluster || max_ctx <= (int64_t)kK4MaxCluster * kK4Warps * kK4Keys * 16);
+  int n = 0;
+  cudaError_t e = k4_resident(1, &n);
+  if (e != cudaSuccess) return e;
+  if (a.cluster) {
+    if (S > kK4MaxCluster) S = kK4MaxCluster;
+    for (; S > 1; --S) {
+      e = k4_resident((int)S, &n);
+      if (e != cudaSuccess) return e;
+      if (n >= groups) break;
+    }
+    a.cluster = S > 1;
+  }
+  a.nsplit = (int)S;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(S * B * Hkv), (unsigned)Z);
+  cfg.blockDim = dim3(kK4Threads);
+  cfg.dynamicSmemBytes = kK4Smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  int na = 0;
+  if (a.cluster) {
+    at[na].id = cudaLaunchAttributeClusterDimension;
+    at[na].val.clusterDim.x = (unsigned)S;
+    at[na].val.clusterDim.y = at[na].val.clusterDim.z = 1;
+    ++na;
+  }
+  const bool legacy = (st == nullptr || st == cudaStreamLegacy || st == cudaStreamPerThread);
+  if (!legacy && pdl_enabled()) {
+    at[na].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[na].val.programmaticStreamSerializationAllowed = 1;
+    ++na;
+  }
+  cfg.attrs = at;
+  cfg.numAttrs = na;
+  e = cudaLaunchKernelEx(&cfg, attention_kv4_kernel, a);
+  if (e != cudaSuccess || a.cluster || S == 1) return e;
+  return launch_attention_combine(a.part, B, T, Hq, Hkv, a.nsplit, out, st);
 }
 
 cudaError_t take_kv4_status(uint32_t* bits) {

@@ -3,118 +3,412 @@
 //
 //   x_v = (z_v - max z) / T,  S = sum_v e^x_v
 //   log p_v = x_v - log S,  H = log S - sum_v e^x_v x_v / S
+//
+// A cluster of CTAs takes a row and keeps it in shared memory, so that logits
+// are read from memory once although they are walked twice: for the maximum,
+// then for the sums.  The entries that may be among the `top` largest are found
+// on the second walk without sorting: the top-th largest of the maxima of
+// groups of threads bounds them from below, and about one entry in a thousand
+// passes.  They are ranked by counting, in each CTA and then in the first.
+// Bound: the logits' bytes from memory for many rows; for one row the three
+// meetings of the cluster.
 #include "sq_serve.h"
+
+#include <mutex>
 
 namespace sq {
 
 static __device__ unsigned int g_lp_status;
 
+constexpr int kLpThreads = 256, kLpWarps = kLpThreads / 32;
+constexpr int kLpChunk = 20480;    // entries of a CTA, where clusters of 16 allow it
+constexpr int kLpMaxCluster = 16;
+constexpr int kLpList = 512;       // candidates of a CTA
+constexpr int kLpParts = 4;        // copies of a CTA's share, each waited for by itself
+
 // Total order of (logit, index): largest logit first, lowest index among
-// equals (-0 equals 0).  Larger keys come first.
-__device__ __forceinline__ uint32_t lp_order16(__half z) {
-  uint32_t b = __half_as_ushort(z);
+// equals (-0 equals 0).  Larger keys come first; 0 is no entry's key.
+__device__ __forceinline__ uint32_t lp_order16(uint32_t b) {
   if (b == 0x8000u) b = 0;
   return b & 0x8000u ? 0xffffu - b : b | 0x8000u;
 }
-__device__ __forceinline__ unsigned long long lp_key(__half z, uint32_t v) {
-  return ((unsigned long long)lp_order16(z) << 32) | (0xffffffffu - v);
+__device__ __forceinline__ float lp_value(uint32_t order) {
+  return __half2float(__ushort_as_half((uint16_t)(order & 0x8000u ? order & 0x7fffu : 0xffffu - order)));
+}
+__device__ __forceinline__ unsigned long long lp_key(uint32_t order, uint32_t v) {
+  return ((unsigned long long)order << 32) | (0xffffffffu - v);
 }
 
-__device__ __forceinline__ unsigned long long lp_block_max(unsigned long long k, unsigned long long* red) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const unsigned long long other = __shfl_xor_sync(0xffffffffu, k, o);
-    k = other > k ? other : k;
+__device__ __forceinline__ uint32_t lp_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void lp_sync(int S) {
+  if (S > 1)
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  else
+    __syncthreads();
+}
+__device__ __forceinline__ uint32_t lp_remote(const void* local, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(local)), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ uint32_t lp_ld32(const void* local, uint32_t rank) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(lp_remote(local, rank)) : "memory");
+  return v;
+}
+__device__ __forceinline__ unsigned long long lp_ld64(const void* local, uint32_t rank) {
+  unsigned long long v;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(lp_remote(local, rank)) : "memory");
+  return v;
+}
+__device__ __forceinline__ float lp_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+struct LpShared {
+  unsigned long long list[kLpList];              // candidates
+  unsigned long long best[kLogprobsMaxTop];      // this CTA's largest, in order
+  uint64_t bar[kLpParts];
+  uint32_t group[32];                            // maxima of this CTA's groups of threads
+  uint32_t hist[256];
+  float sum[2][kLpWarps];
+  float total[2];
+  unsigned int count, equal, overflow, tau, above;
+};
+
+// Ranks n keys of the list by counting; the first k go to `best`.
+template <typename Emit>
+__device__ __forceinline__ void lp_ranked(const unsigned long long* list, int n, int k, Emit emit) {
+  for (int i = threadIdx.x; i < n; i += kLpThreads) {
+    const unsigned long long key = list[i];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += list[j] > key;
+    if (key && rank < k) emit(rank, key);
   }
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = k;
-  __syncthreads();
-  for (int w = 0; w < (int)(blockDim.x >> 5); ++w) k = red[w] > k ? red[w] : k;
-  return k;
 }
 
-// One CTA per row; the alternatives one after another.
-__global__ void __launch_bounds__(256) logprobs_simple_kernel(const LogprobArgs a) {
+// S CTAs (a cluster) a row; dynamic shared memory: the share of the row, at
+// the same place within 16 bytes as in memory.
+__global__ void __launch_bounds__(kLpThreads, 4) logprobs_kernel(const LogprobArgs a, int S, int groups) {
   griddep_wait();
   griddep_launch_dependents();
-  __shared__ unsigned long long red[8];
-  __shared__ float fred[2][8];
-  const int64_t r = blockIdx.x;
+  extern __shared__ __align__(128) uint8_t lp_smem[];
+  __shared__ LpShared s;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const uint32_t rank = S > 1 ? lp_rank() : 0u;
+  const int64_t r = blockIdx.x / (unsigned)S;
+  const int64_t c0 = a.V * rank / S, c1 = a.V * (rank + 1) / S;
+  const int n = (int)(c1 - c0), top = a.top;
   const __half* z = a.z + r * a.V;
-  unsigned long long k = 0;
-  bool bad = false;
-  for (int64_t v = threadIdx.x; v < a.V; v += blockDim.x) {
-    const float f = __half2float(z[v]);
-    bad |= isnan(f) || f == INFINITY;
-    const unsigned long long key = lp_key(z[v], (uint32_t)v);
-    k = key > k ? key : k;
-  }
-  bad = __syncthreads_or(bad);
-  k = lp_block_max(k, red);
-  const float m = __half2float(z[0xffffffffu - (uint32_t)k]);
-  const bool none = !bad && m == -INFINITY;
-  if (bad || none) {
-    if (threadIdx.x == 0) {
-      atomicOr(&g_lp_status, bad ? SQ_DEV_NONFINITE_LOGIT : SQ_DEV_NO_MASS);
-      if (a.logprob) a.logprob[r] = NAN;
-      if (a.entropy) a.entropy[r] = NAN;
+  const __half* src = z + c0;
+  const int shift = (int)((reinterpret_cast<uintptr_t>(src) & 15) >> 1);  // entries before ours in the first 16 bytes
+  const int words = (n + shift + 7) / 8;
+  __half* row = reinterpret_cast<__half*>(lp_smem);  // entry i of the share at row[shift + i]
+
+  // ---- the share: whole 16-byte pieces by bulk copies, ragged ends by hand
+  const int w0 = shift ? 1 : 0, w1 = max((n + shift) / 8, w0);  // whole words
+  if (tid == 0) {
+    for (int p = 0; p < kLpParts; ++p) mbar_init(&s.bar[p], 1);
+    fence_mbar_init();
+    s.count = s.equal = s.overflow = 0;
+    for (int p = 0; p < kLpParts; ++p) {
+      const int b = w0 + (int)((int64_t)(w1 - w0) * p / kLpParts), e = w0 + (int)((int64_t)(w1 - w0) * (p + 1) / kLpParts);
+      mbar_arrive_expect_tx(&s.bar[p], (uint32_t)(e - b) * 16);
+      if (e > b) bulk_g2s(lp_smem + b * 16, src - shift + b * 8, (uint32_t)(e - b) * 16, &s.bar[p]);
     }
-    for (int i = threadIdx.x; i < a.top; i += blockDim.x) {
-      a.top_tokens[r * a.top + i] = -1;
-      a.top_logprobs[r * a.top + i] = NAN;
-    }
-    return;
   }
-  // the largest term is 1; the others apart from it, so that a sure row's
-  // logarithm keeps them
-  const int64_t vmax = 0xffffffffu - (uint32_t)k;
-  float S = 0.0f, E = 0.0f;
-  for (int64_t v = threadIdx.x; v < a.V; v += blockDim.x) {
-    const float x = (__half2float(z[v]) - m) * a.invT;
-    if (v == vmax || x == -INFINITY) continue;
-    const float e = expf(x);
-    S += e;
-    E = fmaf(e, -x, E);
-  }
-  S = warp_sum(S);
-  E = warp_sum(E);
-  if ((threadIdx.x & 31) == 0) {
-    fred[0][threadIdx.x >> 5] = S;
-    fred[1][threadIdx.x >> 5] = E;
+  // ends, and what pads the first and the last word: -inf
+  if (tid < 16) {
+    const int i = tid < 8 ? tid : w1 * 8 + tid - 8;  // place in shared memory
+    if (tid < 8 ? w0 > 0 : w1 < words)
+      row[i] = i >= shift && i < shift + n ? src[i - shift] : __ushort_as_half(0xfc00);
   }
   __syncthreads();
-  S = E = 0.0f;
-  for (int w = 0; w < (int)(blockDim.x >> 5); ++w) {
-    S += fred[0][w];
-    E += fred[1][w];
+
+  // ---- first walk: maxima (a NaN stays one)
+  __half2 mx = __halves2half2(__ushort_as_half(0xfc00), __ushort_as_half(0xfc00));
+  bool late = false;
+  {
+    int part = 0;
+    for (int w = tid; w < words; w += kLpThreads) {
+      // every part up to the one that holds this word
+      while (part < kLpParts && w >= w0 + (int)((int64_t)(w1 - w0) * part / kLpParts)) {
+        late |= !mbar_wait_bounded(&s.bar[part], 0u);
+        ++part;
+      }
+      const uint4 q = reinterpret_cast<const uint4*>(lp_smem)[w];
+      const __half2* h = reinterpret_cast<const __half2*>(&q);
+      mx = __hmax2_nan(__hmax2_nan(mx, __hmax2_nan(h[0], h[1])), __hmax2_nan(h[2], h[3]));
+    }
+    for (; part < kLpParts; ++part) late |= !mbar_wait_bounded(&s.bar[part], 0u);
   }
-  const float lse = log1pf(S);
-  if (threadIdx.x == 0) {
-    if (a.entropy) a.entropy[r] = lse + E / (1.0f + S);
-    if (a.tokens) {
-      const int64_t t = a.tokens[r];
-      const bool ok = t >= 0 && t < a.V;
-      if (!ok) atomicOr(&g_lp_status, SQ_DEV_BAD_TOKEN_ID);
-      a.logprob[r] = ok ? (__half2float(z[t]) - m) * a.invT - lse : NAN;
+  if (late) atomicOr(&g_lp_status, SQ_DEV_TIMEOUT);
+  {
+    const uint32_t b = *reinterpret_cast<const uint32_t*>(&mx);
+    uint32_t o = max(lp_order16(b & 0xffffu), lp_order16(b >> 16));
+    const int span = kLpThreads / groups;  // threads of a group: 8, 16 or 32
+    for (int i = span >> 1; i > 0; i >>= 1) o = max(o, __shfl_xor_sync(0xffffffffu, o, i));
+    if (tid % span == 0) s.group[tid / span] = o;
+  }
+  lp_sync(S);
+  // ---- the row's maximum, and the top-th largest of the groups' maxima
+  uint32_t mo;
+  {
+    const int total = S * groups;  // at most 128
+    uint32_t v = 0;
+    if (tid < total) v = S > 1 ? lp_ld32(&s.group[tid % groups], (uint32_t)(tid / groups)) : s.group[tid];
+    __syncthreads();
+    if (tid < total) s.list[tid] = lp_key(v, (uint32_t)tid);  // (the list is not used yet)
+    __syncthreads();
+    if (tid < total) {
+      const unsigned long long key = s.list[tid];
+      int above = 0;
+      for (int j = 0; j < total; ++j) above += s.list[j] > key;
+      if (above == 0) s.above = v;
+      if (above == (top > 0 ? top - 1 : 0)) s.tau = v;
+    }
+    __syncthreads();
+    mo = s.above;
+  }
+  const float m = lp_value(mo);
+  const bool bad = mo >= 0xfc00u, none = mo == 0x3ffu;  // +inf or NaN; nothing but -inf
+  if (bad || none) {
+    if (rank == 0) {
+      if (tid == 0) {
+        atomicOr(&g_lp_status, bad ? SQ_DEV_NONFINITE_LOGIT : SQ_DEV_NO_MASS);
+        if (a.logprob) a.logprob[r] = NAN;
+        if (a.entropy) a.entropy[r] = NAN;
+      }
+      if (tid < top) {
+        a.top_tokens[r * top + tid] = -1;
+        a.top_logprobs[r * top + tid] = NAN;
+      }
+    }
+    lp_sync(S);  // (no CTA leaves while another reads its maxima)
+    return;
+  }
+
+  // Candidates of one word: entries above tau, and of those equal to it the
+  // first `top` of a warp, whose words come in rising order.
+  unsigned int ties = 0;  // this warp's
+  auto offer = [&](const uint16_t* h, int w, bool any, uint32_t tau) {
+    if (!__any_sync(0xffffffffu, any)) return;
+    unsigned int mine = 0, hits = 0;
+    uint32_t o[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int i = w * 8 + e - shift;
+      o[e] = any && i >= 0 && i < n ? lp_order16(h[e]) : 0u;
+      mine += o[e] == tau;
+      hits |= (o[e] > tau ? 1u : 0u) << e;
+    }
+    unsigned int before = mine;  // ties of lower lanes
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const unsigned int v = __shfl_up_sync(0xffffffffu, before, d);
+      if (lane >= d) before += v;
+    }
+    const unsigned int all = __shfl_sync(0xffffffffu, before, 31);
+    before -= mine;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      bool take = (hits >> e) & 1;
+      if (o[e] == tau && o[e]) take = ties + before++ < (unsigned)top;
+      if (take) {
+        const unsigned int at = atomicAdd(&s.count, 1u);
+        if (at < kLpList) s.list[at] = lp_key(o[e], (uint32_t)(c0 + w * 8 + e - shift));
+      }
+    }
+    ties += all;
+  };
+
+  // ---- second walk: the sums, apart from entries equal to the maximum (their
+  // terms are ones, counted: a sure row's logarithm keeps what is left)
+  uint32_t tau = s.tau;
+  const float sc = a.invT * 1.4426950408889634f;
+  float S0 = 0.0f, S1 = 0.0f, E0 = 0.0f, E1 = 0.0f;
+  unsigned int ones = 0;
+  const __half tau_h = __float2half_rn(lp_value(tau));
+  const __half2 tau2 = __halves2half2(tau_h, tau_h);
+  for (int wb = 0; wb < words; wb += kLpThreads) {
+    const int w = wb + tid;
+    uint4 q = make_uint4(0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u);
+    if (w < words) q = reinterpret_cast<const uint4*>(lp_smem)[w];
+    const __half2* h = reinterpret_cast<const __half2*>(&q);
+    const __half2 wm = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    const bool any = w < words && !__hblt2(wm, tau2);  // an entry at tau or above
+    const bool near = any && !__hblt2(wm, __half2half2(__float2half_rn(m)));  // at the maximum
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 f = __half22float2(h[e]);
+      // (clamped: -inf has no weight, and 2^-150 is zero)
+      float y0 = fmaxf((f.x - m) * sc, -150.0f), y1 = fmaxf((f.y - m) * sc, -150.0f);
+      float e0 = lp_ex2(y0), e1 = lp_ex2(y1);
+      if (near) {
+        ones += (f.x == m) + (f.y == m);
+        e0 = f.x == m ? 0.0f : e0;
+        e1 = f.y == m ? 0.0f : e1;
+      }
+      S0 += e0;
+      S1 += e1;
+      E0 = fmaf(e0, y0, E0);
+      E1 = fmaf(e1, y1, E1);
+    }
+    if (top > 0) offer(reinterpret_cast<const uint16_t*>(&q), w, any, tau);
+  }
+  S0 = warp_sum(S0 + S1);
+  E0 = warp_sum(E0 + E1);
+  ones = __reduce_add_sync(0xffffffffu, ones);
+  if (lane == 0) {
+    s.sum[0][warp] = S0;
+    s.sum[1][warp] = E0;
+    if (ones) atomicAdd(&s.equal, ones);
+  }
+  __syncthreads();
+  if (tid < 2) {
+    float t = 0.0f;
+    for (int i = 0; i < kLpWarps; ++i) t += s.sum[tid][i];
+    s.total[tid] = t;
+  }
+  if (tid == 0) s.overflow = s.count > kLpList;
+  lp_sync(S);
+
+  // ---- rarely (rows in order, say) more pass than the list holds: the top-th
+  // largest logit itself, by two walks that count its upper and its lower byte
+  if (top > 0) {
+    bool over = false;
+    for (int i = 0; i < S; ++i) over |= (S > 1 ? lp_ld32(&s.overflow, (uint32_t)i) : s.overflow) != 0;
+    if (over) {
+      uint32_t prefix = 0;
+      unsigned int above = 0;  // entries above the bytes found so far
+      for (int byte = 1; byte >= 0; --byte) {
+        lp_sync(S);  // (the others have read the last counts)
+        s.hist[tid] = 0;
+        __syncthreads();
+        for (int i = tid; i < n; i += kLpThreads) {
+          const uint32_t o = lp_order16(__half_as_ushort(row[shift + i]));
+          if (byte == 1 || (o >> 8) == prefix) atomicAdd(&s.hist[byte == 1 ? o >> 8 : o & 255u], 1u);
+        }
+        lp_sync(S);
+        unsigned int c = 0;
+        for (int i = 0; i < S; ++i) c += S > 1 ? lp_ld32(&s.hist[tid], (uint32_t)i) : s.hist[tid];
+        __syncthreads();
+        s.list[tid] = c;
+        __syncthreads();
+        unsigned int over_me = above;
+        for (int j = tid + 1; j < 256; ++j) over_me += (unsigned int)s.list[j];
+        if (over_me < (unsigned)top && over_me + c >= (unsigned)top) {
+          s.tau = byte == 1 ? (uint32_t)tid : (prefix << 8) | (uint32_t)tid;
+          s.above = over_me;
+        }
+        __syncthreads();
+        prefix = s.tau;
+        above = s.above;
+      }
+      tau = prefix;
+      if (tid == 0) s.count = 0;
+      ties = 0;
+      __syncthreads();
+      for (int wb = 0; wb < words; wb += kLpThreads) {
+        const int w = wb + tid;
+        uint4 q = make_uint4(0, 0, 0, 0);
+        if (w < words) q = reinterpret_cast<const uint4*>(lp_smem)[w];
+        offer(reinterpret_cast<const uint16_t*>(&q), w, w < words, tau);
+      }
+      __syncthreads();
+    }
+    // this CTA's largest, then the row's
+    if (tid < top) s.best[tid] = 0;
+    __syncthreads();
+    lp_ranked(s.list, min((int)s.count, kLpList), top, [&](int i, unsigned long long key) { s.best[i] = key; });
+    lp_sync(S);
+  }
+  if (rank == 0) {
+    float t0 = 0.0f, t1 = 0.0f;
+    unsigned int eq = 0;
+    for (int i = 0; i < S; ++i) {
+      t0 += S > 1 ? __uint_as_float(lp_ld32(&s.total[0], (uint32_t)i)) : s.total[0];
+      t1 += S > 1 ? __uint_as_float(lp_ld32(&s.total[1], (uint32_t)i)) : s.total[1];
+      eq += S > 1 ? lp_ld32(&s.equal, (uint32_t)i) : s.equal;
+    }
+    const float rest = t0 + (float)(eq - 1);
+    const float lse = log1pf(rest);
+    if (tid == 0) {
+      if (a.entropy) a.entropy[r] = lse - t1 * 0.6931471805599453f / (1.0f + rest);
+      if (a.tokens) {
+        const int64_t t = a.tokens[r];
+        const bool ok = t >= 0 && t < a.V;
+        if (!ok) atomicOr(&g_lp_status, SQ_DEV_BAD_TOKEN_ID);
+        a.logprob[r] = ok ? (__half2float(z[t]) - m) * a.invT - lse : NAN;
+      }
+    }
+    if (top > 0) {
+      const int all = S * top;  // at most kLpList
+      for (int i = tid; i < all; i += kLpThreads)
+        s.list[i] = S > 1 ? lp_ld64(&s.best[i % top], (uint32_t)(i / top)) : s.best[i];
+      __syncthreads();
+      lp_ranked(s.list, all, top, [&](int i, unsigned long long key) {
+        a.top_tokens[r * top + i] = (int32_t)(0xffffffffu - (uint32_t)key);
+        a.top_logprobs[r * top + i] = (lp_value((uint32_t)(key >> 32)) - m) * a.invT - lse;
+      });
     }
   }
-  for (int i = 0; i < a.top; ++i) {
-    const int64_t v = 0xffffffffu - (uint32_t)k;
-    if (threadIdx.x == 0) {
-      a.top_tokens[r * a.top + i] = (int32_t)v;
-      a.top_logprobs[r * a.top + i] = (__half2float(z[v]) - m) * a.invT - lse;
-    }
-    unsigned long long n = 0;
-    for (int64_t u = threadIdx.x; u < a.V; u += blockDim.x) {
-      const unsigned long long key = lp_key(z[u], (uint32_t)u);
-      if (key < k && key > n) n = key;
-    }
-    k = lp_block_max(n, red);
-  }
+  lp_sync(S);  // no CTA leaves while the first reads its results
 }
 
+// CTAs a row: shares of kLpChunk entries; more of them where rows alone leave
+// SMs idle, down to shares of 4096.
 cudaError_t launch_logprobs(const LogprobArgs& a, cudaStream_t st) {
-  return launch_pdl(logprobs_simple_kernel, dim3((unsigned)a.R), dim3(256), 0, st, a);
+  static std::mutex mu;
+  static bool ready[64] = {false};
+  constexpr int kMaxSmem = 2 * ((1 << 20) / kLpMaxCluster + 16);
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  {
+    std::lock_guard<std::mutex> lock(mu);
+    if (!ready[dev]) {
+      e = cudaFuncSetAttribute(logprobs_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
+      if (e == cudaSuccess) e = cudaFuncSetAttribute(logprobs_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+      if (e != cudaSuccess) return e;
+      ready[dev] = true;
+    }
+  }
+  int64_t S = (a.V + kLpChunk - 1) / kLpChunk;
+  if (S > kLpMaxCluster) S = kLpMaxCluster;
+  while (2 * S <= kLpMaxCluster && 2 * S * a.R <= device_sm_count() && a.V / (2 * S) >= 4096) S *= 2;
+  const int64_t share = (a.V + S - 1) / S;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(a.R * S));
+  cfg.blockDim = dim3(kLpThreads);
+  cfg.dynamicSmemBytes = (size_t)((share + 15) / 8 * 16);
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  int na = 0;
+  if (S > 1) {
+    at[na].id = cudaLaunchAttributeClusterDimension;
+    at[na].val.clusterDim.x = (unsigned)S;
+    at[na].val.clusterDim.y = at[na].val.clusterDim.z = 1;
+    ++na;
+  }
+  const bool legacy = (st == nullptr || st == cudaStreamLegacy || st == cudaStreamPerThread);
+  if (!legacy && pdl_enabled()) {
+    at[na].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[na].val.programmaticStreamSerializationAllowed = 1;
+    ++na;
+  }
+  cfg.attrs = at;
+  cfg.numAttrs = na;
+  // groups of threads whose maxima are kept: 32 a row at least
+  const int groups = S == 1 ? 32 : S < 4 ? 16 : 8;
+  return cudaLaunchKernelEx(&cfg, logprobs_kernel, a, (int)S, groups);
 }
 
 cudaError_t take_logprobs_status(uint32_t* bits) {

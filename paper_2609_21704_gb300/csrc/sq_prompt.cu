@@ -250,23 +250,7 @@ __global__ void __launch_bounds__(kPrPrepThreads) prompt_prepare_kernel(
   __shared__ RopeCS cs[kPrPrepRows][kHeadDim / 2];
   __shared__ int seq[kPrPrepRows], pos[kPrPrepRows];
   const int64_t row0 = (int64_t)(blockIdx.x - 1) * kPrPrepRows;
-  if (tid < kPrPrepRows) seq[tid] = -1;
-  __syncthreads();
-  bool bad = false;
-  for (int b = tid; b < pk.B; b += kPrPrepThreads) {
-    const int lo = pk.offsets[b], hi = pk.offsets[b + 1];
-    bad |= lo < 0 || hi < lo || (int64_t)hi > pk.N;
-#pragma unroll
-    for (int i = 0; i < kPrPrepRows; ++i)
-      if (lo <= row0 + i && row0 + i < hi) {
-        const int64_t p0 = pk.pos0[b];
-        const bool ok = p0 >= 0 && p0 + (hi - lo) <= pk.max_ctx;
-        seq[i] = b;
-        pos[i] = ok ? (int)(p0 + (row0 + i - lo)) : -1;
-        if (!ok) atomicOr(&g_prompt_status, SQ_DEV_BAD_POSITION);
-      }
-  }
-  if (__syncthreads_or(bad)) return;
+  if (packed_rows<kPrPrepRows>(pk, row0, seq, pos, &g_prompt_status)) return;
   {
     const int i = tid / (kHeadDim / 2), d = tid % (kHeadDim / 2);
     // (eight neighbouring dimensions lie 128 bytes apart, so that the lanes of a head read neighbours)
