@@ -429,8 +429,8 @@ SQ_API sq_status sq_spec_drafts(const int32_t* samples, const int32_t* last2, in
  *   out[row] = sum_{j <= pos} p_j v_j / sum_j p_j,
  *   p_j = exp(q . k_j / sqrt(D))
  * over the cache, query head h against key/value head h / (Hq / Hkv), out
- * fp16 [N, Hq * D].  Rotated queries and keys are rounded to fp16 once,
- * correctly; products are exact; sums and the softmax's statistics are fp32;
+ * fp16 [N, Hq * D].  Rotated keys are rounded to fp16 once, correctly,
+ * rotated queries from fp32; products are exact; sums and the softmax's statistics are fp32;
  * a probability relative to its row's maximum is rounded to fp16 for its
  * product with the value (its sum is not).  What lies in the caches behind a
  * token's position, infinities and NaN included, has no effect on its row;

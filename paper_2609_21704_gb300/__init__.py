@@ -13,6 +13,7 @@ Adaptive LLM Inference" (Sec. III-A variants, Sec. III-D pipeline).
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -50,6 +51,7 @@ _P = ctypes.c_void_p
 _I64 = ctypes.c_int64
 _INT = ctypes.c_int
 _SIZE = ctypes.c_size_t
+_F16, _F32, _I32, _U8 = torch.float16, torch.float32, torch.int32, torch.uint8
 _SIGS = {
     "sq_last_error": (ctypes.c_char_p, []),
     "sq_status_string": (ctypes.c_char_p, [_INT]),
@@ -146,8 +148,15 @@ def _ptr(t):
     return t.data_ptr()
 
 
+# The current stream's handle without a Stream object around it (0.1 us against
+# 2.9 us of a call's 10 to 20 on the host).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream):
     if stream is None:
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream
@@ -350,27 +359,57 @@ def sq_spec_drafts(samples, last2, verify_tokens, draft, stream=None) -> None:
                                                    _ptr(verify_tokens), _ptr(draft), _stream(stream)))
 
 
-def _want(what: str, t, dtype, *shape):
-    """t is a tensor of this type and shape (None: any size) on the current device."""
+def _args(*wanted):
+    """The device pointers of (name, tensor, dtype, shape) arguments: types and
+    shapes first, then that all lie, contiguous, on the current device."""
+    for what, t, dtype, shape in wanted:
+        if t is None:
+            continue
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{what}: expected a torch.Tensor")
+        if t.dtype is not dtype:
+            raise TypeError(f"{what}: expected {dtype}, got {t.dtype}")
+        if t.shape != shape:
+            raise ValueError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    out = []
+    dev = None
+    for what, t, _, _ in wanted:
+        if t is None:
+            out.append(None)
+            continue
+        d = t.get_device()
+        if d != dev:
+            if d < 0:
+                raise ValueError(f"{what}: tensor must live on a CUDA device")
+            if dev is not None:
+                raise ValueError(f"{what}: on cuda:{d}, other arguments on cuda:{dev}")
+            dev = d
+        if not t.is_contiguous():
+            raise ValueError(f"{what}: tensor must be contiguous")
+        out.append(t.data_ptr())
+    if dev is not None and dev != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on cuda:{dev}, the current device is cuda:{torch.cuda.current_device()}")
+    return out
+
+
+def _size(what: str, t, dims: int, i: int) -> int:
+    """Size i of a tensor of `dims` dimensions."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{what}: expected a torch.Tensor")
-    if t.dtype != dtype:
-        raise TypeError(f"{what}: expected {dtype}, got {t.dtype}")
-    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
-        raise ValueError(f"{what}: expected shape {shape}, got {tuple(t.shape)}")
-    if t.is_cuda and t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{what}: on {t.device}, but the current device is {torch.cuda.current_device()}")
-    return t
+    if t.dim() != dims:
+        raise ValueError(f"{what}: expected {dims} dimensions, got shape {tuple(t.shape)}")
+    return t.shape[i]
 
 
-def sq_attention_prompt_workspace_bytes(B, N, Hq, Hkv, max_ctx) -> int:
-    return int(load().sq_attention_prompt_workspace_bytes(B, N, Hq, Hkv, 128, max_ctx))
-
-
-def _heads(qkv, Hq, Hkv):
+def _check_heads(Hq: int, Hkv: int) -> int:
     if Hq < 1 or Hkv < 1 or Hq % Hkv:
         raise ValueError(f"Hq = {Hq} must be a positive multiple of Hkv = {Hkv}")
-    return _want("qkv", qkv, torch.float16, None, (Hq + 2 * Hkv) * 128).shape[0]
+    return (Hq + 2 * Hkv) * 128
+
+
+@functools.lru_cache(maxsize=256)
+def sq_attention_prompt_workspace_bytes(B, N, Hq, Hkv, max_ctx) -> int:
+    return int(load().sq_attention_prompt_workspace_bytes(B, N, Hq, Hkv, 128, max_ctx))
 
 
 def sq_attention_prompt(qkv, offsets, Hq, Hkv, pos0, theta, k_cache, v_cache, out, workspace,
@@ -378,56 +417,54 @@ def sq_attention_prompt(qkv, offsets, Hq, Hkv, pos0, theta, k_cache, v_cache, ou
     """Causal GQA attention of packed prompts and the append of their keys and
     values: qkv fp16 [N, (Hq+2Hkv)*128], offsets int32 [B+1] (sequence b: rows
     offsets[b] .. offsets[b+1]-1, at positions pos0[b] ..), caches fp16
-    [B, Hkv, max_ctx, 128], out fp16 [N, Hq*128]."""
-    N = _heads(qkv, Hq, Hkv)
-    B = _want("pos0", pos0, torch.int32, None).shape[0]
-    _want("offsets", offsets, torch.int32, B + 1)
-    C = _want("k_cache", k_cache, torch.float16, B, Hkv, None, 128).shape[2]
-    _want("v_cache", v_cache, torch.float16, B, Hkv, C, 128)
-    _want("out", out, torch.float16, N, Hq * 128)
-    _check("sq_attention_prompt", load().sq_attention_prompt(
-        _ptr(qkv), N, _ptr(offsets), B, Hq, Hkv, 128, _ptr(pos0), float(theta), _ptr(k_cache), _ptr(v_cache), C,
-        _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+    [B, Hkv, max_ctx, 128], out fp16 [N, Hq*128], workspace uint8."""
+    N, B, C = _size("qkv", qkv, 2, 0), _size("pos0", pos0, 1, 0), _size("k_cache", k_cache, 4, 2)
+    cache = (B, Hkv, C, 128)
+    x, off, p0, k, v, o, ws = _args(
+        ("qkv", qkv, _F16, (N, _check_heads(Hq, Hkv))), ("offsets", offsets, _I32, (B + 1,)), ("pos0", pos0, _I32, (B,)),
+        ("k_cache", k_cache, _F16, cache), ("v_cache", v_cache, _F16, cache), ("out", out, _F16, (N, Hq * 128)),
+        ("workspace", workspace, _U8, (_size("workspace", workspace, 1, 0),)))
+    _check("sq_attention_prompt", load().sq_attention_prompt(x, N, off, B, Hq, Hkv, 128, p0, theta, k, v, C, o, ws,
+                                                             workspace.shape[0], _stream(stream)))
 
 
 def _kv4(B, Hkv, k_codes, k_params, v_codes, v_params):
-    C = _want("k_codes", k_codes, torch.uint8, B, Hkv, None, 64).shape[2]
-    _want("k_params", k_params, torch.float16, B, Hkv, C, 2)
-    if v_codes.numel() != k_codes.numel():
-        raise ValueError(f"v_codes: expected {k_codes.numel()} bytes, got {v_codes.numel()}")
-    _want("v_codes", v_codes, torch.uint8, *v_codes.shape)
-    _want("v_params", v_params, torch.float16, B, Hkv, C, 2)
-    return C, (_ptr(k_codes), _ptr(k_params), _ptr(v_codes), _ptr(v_params))
+    C = _size("k_codes", k_codes, 4, 2)
+    if isinstance(v_codes, torch.Tensor) and v_codes.dim() == 4 and v_codes.shape[3] == 128:
+        pairs = (B, Hkv, C // 2, 128)
+    else:
+        pairs = (B, Hkv, C, 64)  # (the same bytes)
+    return C, (("k_codes", k_codes, _U8, (B, Hkv, C, 64)), ("k_params", k_params, _F16, (B, Hkv, C, 2)),
+               ("v_codes", v_codes, _U8, pairs), ("v_params", v_params, _F16, (B, Hkv, C, 2)))
 
 
 def sq_kv4_append(qkv, Hq, Hkv, pos0, theta, k_codes, k_params, v_codes, v_params, offsets=None,
                   stream=None) -> None:
     """The new tokens' keys (rotated) and values into the 4-bit caches: codes
-    uint8 [B, Hkv, max_ctx, 64] (v_codes in pairs of positions, see the C
+    uint8 [B, Hkv, max_ctx, 64] (v_codes [B, Hkv, max_ctx / 2, 128], or the
+    same bytes as [.., max_ctx, 64]: they lie in pairs of positions, see the C
     declaration), params fp16 [B, Hkv, max_ctx, 2]; rows of qkv as for
     sq_attention_prompt, or without offsets N / B of each sequence."""
-    N = _heads(qkv, Hq, Hkv)
-    B = _want("pos0", pos0, torch.int32, None).shape[0]
-    if offsets is not None:
-        _want("offsets", offsets, torch.int32, B + 1)
-    C, ptrs = _kv4(B, Hkv, k_codes, k_params, v_codes, v_params)
-    _check("sq_kv4_append", load().sq_kv4_append(_ptr(qkv), N, _ptr(offsets), B, Hq, Hkv, 128, _ptr(pos0),
-                                                 float(theta), *ptrs, C, _stream(stream)))
+    N, B = _size("qkv", qkv, 2, 0), _size("pos0", pos0, 1, 0)
+    C, cache = _kv4(B, Hkv, k_codes, k_params, v_codes, v_params)
+    x, off, p0, kc, kp, vc, vp = _args(("qkv", qkv, _F16, (N, _check_heads(Hq, Hkv))), ("offsets", offsets, _I32, (B + 1,)),
+                                       ("pos0", pos0, _I32, (B,)), *cache)
+    _check("sq_kv4_append", load().sq_kv4_append(x, N, off, B, Hq, Hkv, 128, p0, theta, kc, kp, vc, vp, C,
+                                                 _stream(stream)))
 
 
 def sq_kv4_unpack(k_codes, k_params, v_codes, v_params, first, last, k_cache, v_cache, stream=None) -> None:
     """Positions first[b] .. last[b]-1 of the 4-bit caches as fp16 into
     k_cache, v_cache [B, Hkv, max_ctx, 128]."""
-    B = _want("first", first, torch.int32, None).shape[0]
-    _want("last", last, torch.int32, B)
-    Hkv = _want("k_cache", k_cache, torch.float16, B, None, None, 128).shape[1]
-    C, ptrs = _kv4(B, Hkv, k_codes, k_params, v_codes, v_params)
-    _want("k_cache", k_cache, torch.float16, B, Hkv, C, 128)
-    _want("v_cache", v_cache, torch.float16, B, Hkv, C, 128)
-    _check("sq_kv4_unpack", load().sq_kv4_unpack(*ptrs, B, Hkv, 128, C, _ptr(first), _ptr(last), _ptr(k_cache),
-                                                 _ptr(v_cache), _stream(stream)))
+    B, Hkv = _size("first", first, 1, 0), _size("k_cache", k_cache, 4, 1)
+    C, cache = _kv4(B, Hkv, k_codes, k_params, v_codes, v_params)
+    kc, kp, vc, vp, lo, hi, k, v = _args(*cache, ("first", first, _I32, (B,)), ("last", last, _I32, (B,)),
+                                         ("k_cache", k_cache, _F16, (B, Hkv, C, 128)),
+                                         ("v_cache", v_cache, _F16, (B, Hkv, C, 128)))
+    _check("sq_kv4_unpack", load().sq_kv4_unpack(kc, kp, vc, vp, B, Hkv, 128, C, lo, hi, k, v, _stream(stream)))
 
 
+@functools.lru_cache(maxsize=256)
 def sq_attention_kv4_workspace_bytes(B, T, Hq, Hkv, max_ctx) -> int:
     return int(load().sq_attention_kv4_workspace_bytes(B, T, Hq, Hkv, 128, max_ctx))
 
@@ -435,15 +472,13 @@ def sq_attention_kv4_workspace_bytes(B, T, Hq, Hkv, max_ctx) -> int:
 def sq_attention_kv4(qkv, B, T, Hq, Hkv, pos0, theta, k_codes, k_params, v_codes, v_params, out, workspace,
                      stream=None) -> None:
     """out fp16 [B*T, Hq*128] = causal GQA attention of T new tokens a sequence
-    (already appended) over the 4-bit caches."""
-    if _heads(qkv, Hq, Hkv) != B * T:
-        raise ValueError(f"qkv: expected {B * T} rows, got {qkv.shape[0]}")
-    _want("pos0", pos0, torch.int32, B)
-    C, ptrs = _kv4(B, Hkv, k_codes, k_params, v_codes, v_params)
-    _want("out", out, torch.float16, B * T, Hq * 128)
-    _check("sq_attention_kv4", load().sq_attention_kv4(
-        _ptr(qkv), B, T, Hq, Hkv, 128, _ptr(pos0), float(theta), *ptrs, C, _ptr(out), _ptr(workspace),
-        workspace.numel() * workspace.element_size(), _stream(stream)))
+    (already appended) over the 4-bit caches; workspace uint8."""
+    C, cache = _kv4(B, Hkv, k_codes, k_params, v_codes, v_params)
+    x, p0, kc, kp, vc, vp, o, ws = _args(
+        ("qkv", qkv, _F16, (B * T, _check_heads(Hq, Hkv))), ("pos0", pos0, _I32, (B,)), *cache,
+        ("out", out, _F16, (B * T, Hq * 128)), ("workspace", workspace, _U8, (_size("workspace", workspace, 1, 0),)))
+    _check("sq_attention_kv4", load().sq_attention_kv4(x, B, T, Hq, Hkv, 128, p0, theta, kc, kp, vc, vp, C, o, ws,
+                                                       workspace.shape[0], _stream(stream)))
 
 
 def sq_logprobs(z, temperature, tokens=None, logprob=None, entropy=None, top_tokens=None, top_logprobs=None,
@@ -451,20 +486,15 @@ def sq_logprobs(z, temperature, tokens=None, logprob=None, entropy=None, top_tok
     """Rows of fp16 logits z [R, V]: logprob fp32 [R] of tokens int32 [R], the
     entropy fp32 [R], and the largest entries' top_tokens int32 [R, top] and
     top_logprobs fp32 [R, top]; what is None is left out."""
-    R, V = _want("z", z, torch.float16, None, None).shape
-    if tokens is not None:
-        _want("tokens", tokens, torch.int32, R)
-    for what, t in (("logprob", logprob), ("entropy", entropy)):
-        if t is not None:
-            _want(what, t, torch.float32, R)
-    top = 0
-    if top_tokens is not None:
-        top = _want("top_tokens", top_tokens, torch.int32, R, None).shape[1]
-    if top_logprobs is not None or top:
-        _want("top_logprobs", top_logprobs, torch.float32, R, top)
-    _check("sq_logprobs", load().sq_logprobs(_ptr(z), R, V, float(temperature), _ptr(tokens), _ptr(logprob),
-                                             _ptr(entropy), top, _ptr(top_tokens) if top else None,
-                                             _ptr(top_logprobs) if top else None, _stream(stream)))
+    R, V = _size("z", z, 2, 0), z.shape[1]
+    if (top_tokens is None) != (top_logprobs is None):
+        raise TypeError("top_tokens and top_logprobs go together")
+    top = 0 if top_tokens is None else _size("top_tokens", top_tokens, 2, 1)
+    pz, pt, pl, pe, tt, tl = _args(("z", z, _F16, (R, V)), ("tokens", tokens, _I32, (R,)),
+                                   ("logprob", logprob, _F32, (R,)), ("entropy", entropy, _F32, (R,)),
+                                   ("top_tokens", top_tokens, _I32, (R, top)),
+                                   ("top_logprobs", top_logprobs, _F32, (R, top)))
+    _check("sq_logprobs", load().sq_logprobs(pz, R, V, temperature, pt, pl, pe, top, tt, tl, _stream(stream)))
 
 
 def sq_accept_workspace_bytes(B: int, K: int, V: int) -> int:

@@ -20,91 +20,105 @@ namespace sq {
 
 static __device__ unsigned int g_kv4_status;
 
-// Codes of one row whose lane holds the fp16 values x[4]; par: scale and lowest.
-// A quotient comes from the reciprocal (within 2^-19 of the quotient: it is at
-// most 15); only where that leaves the rounding open is it divided.
-__device__ __forceinline__ uint32_t kv4_encode(const float x[4], uint32_t& par, bool& fine) {
-  float lo = fminf(fminf(x[0], x[1]), fminf(x[2], x[3]));
-  float hi = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-  bool ok = true;
+// Codes (nibble e: x[e]) of one row whose 16 lanes hold eight fp16 values each;
+// par: scale and lowest.  A quotient comes from the reciprocal (within 2^-19 of
+// the quotient: it is at most 15); only where that leaves the rounding open is
+// it divided.
+__device__ __forceinline__ uint32_t kv4_encode(const float x[8], uint32_t& par, bool& fine) {
+  float lo = x[0], hi = x[0], sum = x[0] - x[0];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) ok = ok && isfinite(x[e]);
-  fine = __all_sync(0xffffffffu, ok);
-  if (!fine) {
-    par = 0x7fff7fffu;  // NaN: everything read from this row is
-    return 0;
+  for (int e = 1; e < 8; ++e) {
+    lo = fminf(lo, x[e]);
+    hi = fmaxf(hi, x[e]);
+    sum += x[e] - x[e];  // (0, or NaN where one is not finite)
   }
-  lo = -warp_max(-lo);
-  hi = warp_max(hi);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) {
+    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  }
+  fine = sum == 0.0f;
   lo = lo == 0.0f ? 0.0f : lo;
   __half s16 = __float2half_rn(__fdiv_rn(__fsub_rn(hi, lo), 15.0f));
   if (__half_as_ushort(s16) == 0 && hi > lo) s16 = __ushort_as_half(1);
   const float s = __half2float(s16);
   par = (uint32_t)__half_as_ushort(s16) | ((uint32_t)__half_as_ushort(__float2half_rn(lo)) << 16);
-  if (s == 0.0f) return 0;
+  if (!fine) par = 0x7fff7fffu;  // NaN: everything read from this row is
+  if (!fine || s == 0.0f) return 0;
   const float inv = __frcp_rn(s);
   uint32_t w = 0;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
+  for (int e = 0; e < 8; ++e) {
     const float d = __fsub_rn(x[e], lo);
     const float q = d * inv;
     float c = rintf(q);
     if (fabsf(fabsf(q - c) - 0.5f) < 1e-5f) c = rintf(__fdiv_rn(d, s));
-    w |= (uint32_t)fminf(fmaxf(c, 0.0f), 15.0f) << (4 * e);
+    w |= (uint32_t)fminf(c, 15.0f) << (4 * e);
   }
   return w;
 }
 
-// One CTA per kAppendRows rows (their rotation tables are shared by all heads),
-// a warp per (row, key/value head, key or value); a warp reads 256 contiguous
-// bytes, and the table's two entries of a lane lie together.
-constexpr int kAppendRows = 4, kAppendThreads = 256;
+__device__ __forceinline__ void kv4_floats4(uint2 v, float* x) {
+  const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&v.x));
+  const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&v.y));
+  x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
+}
+
+// One CTA per R rows, which share their rotation tables; 16 lanes a (row,
+// key/value head, key or value).  A lane's eight key dimensions are 4u .. 4u + 3
+// and 64 more, its rotation entries four that lie 16 entries apart.  R = 1 while
+// that leaves no SM without a CTA, as a decode step: what counts is one row's
+// chain of operations.
+constexpr int kAppendThreads = 256;
+template <int R>
 __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(const __half* __restrict__ qkv, const Packed pk,
                                                                     int Hq, int Hkv, const RopeFreq rf,
                                                                     const KV4Cache c) {
   griddep_wait();
   griddep_launch_dependents();
-  __shared__ RopeCS cs[kAppendRows][kHeadDim / 2];
-  __shared__ int seq[kAppendRows], pos[kAppendRows];
-  const int64_t row0 = (int64_t)blockIdx.x * kAppendRows;
-  const int tid = threadIdx.x, lane = tid & 31;
-  if (packed_rows<kAppendRows>(pk, row0, seq, pos, &g_kv4_status)) return;
-  {
+  __shared__ RopeCS cs[R][kHeadDim / 2];  // dimension d at (d % 4) * 16 + d / 4
+  __shared__ int seq[R], pos[R];
+  const int64_t row0 = (int64_t)blockIdx.x * R;
+  const int tid = threadIdx.x;
+  if (packed_rows<R>(pk, row0, seq, pos, &g_kv4_status)) return;
+  if (tid < R * (kHeadDim / 2)) {
     const int i = tid / (kHeadDim / 2), d = tid % (kHeadDim / 2);
-    if (seq[i] >= 0 && pos[i] >= 0) cs[i][d] = rope_cs_pair(pos[i], rf.f[d]);
+    if (seq[i] >= 0 && pos[i] >= 0) cs[i][(d & 3) * 16 + (d >> 2)] = rope_cs_pair(pos[i], rf.f[d]);
   }
   __syncthreads();
-  for (int j = tid >> 5; j < kAppendRows * 2 * Hkv; j += kAppendThreads >> 5) {
-    const int r = j / (2 * Hkv), i = j - r * 2 * Hkv;
-    if (seq[r] < 0 || pos[r] < 0) continue;
+  const int u = tid & 15, per = 2 * Hkv;
+  // (the lanes of a warp stay together: R 2 Hkv rows are an even number)
+  for (int j = tid >> 4; j < R * per; j += kAppendThreads / 16) {
+    const int r = R == 1 ? 0 : j / per, i = j - r * per;
+    const bool mine = seq[r] >= 0 && pos[r] >= 0;
     const bool val = i >= Hkv;
-    const int h = val ? i - Hkv : i;
-    const int64_t slot = ((int64_t)seq[r] * Hkv + h) * pk.max_ctx + pos[r];
-    const __half* src = qkv + ((row0 + r) * (int64_t)(Hq + 2 * Hkv) + Hq + i) * kHeadDim;
-    float x[4];
-    bool fine;
-    uint32_t par, w;
-    if (val) {  // dimensions 4 lane ..
-      const uint2 v = reinterpret_cast<const uint2*>(src)[lane];
-      const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&v.x));
-      const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&v.y));
-      x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
-      w = kv4_encode(x, par, fine);
-      uint16_t* dst = reinterpret_cast<uint16_t*>(c.vc + (slot >> 1) * kHeadDim);
-      dst[2 * lane + (slot & 1)] = (uint16_t)w;
-    } else {  // dimensions 2 lane, 2 lane + 1 and 64 more
-      const float2 a = __half22float2(reinterpret_cast<const __half2*>(src)[lane]);
-      const float2 b = __half22float2(reinterpret_cast<const __half2*>(src)[lane + 32]);
-      const RopeCS r0 = cs[r][2 * lane], r1 = cs[r][2 * lane + 1];
-      x[0] = __half2float(__float2half_rn(rope_dot(a.x, r0.c, -b.x, r0.s)));
-      x[1] = __half2float(__float2half_rn(rope_dot(a.y, r1.c, -b.y, r1.s)));
-      x[2] = __half2float(__float2half_rn(rope_dot(b.x, r0.c, a.x, r0.s)));
-      x[3] = __half2float(__float2half_rn(rope_dot(b.y, r1.c, a.y, r1.s)));
-      w = kv4_encode(x, par, fine);
-      c.kc[slot * (kHeadDim / 2) + lane] = (uint8_t)w;
-      c.kc[slot * (kHeadDim / 2) + lane + 32] = (uint8_t)(w >> 8);
+    const int64_t slot = mine ? ((int64_t)seq[r] * Hkv + (val ? i - Hkv : i)) * pk.max_ctx + pos[r] : 0;
+    const uint2* src =
+        reinterpret_cast<const uint2*>(qkv + ((row0 + r) * (int64_t)(Hq + per) + Hq + i) * kHeadDim);
+    float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    if (mine) {
+      kv4_floats4(src[val ? 2 * u : u], x);
+      kv4_floats4(src[val ? 2 * u + 1 : u + 16], x + 4);
+      if (!val) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const RopeCS t = cs[r][e * 16 + u];
+          const float a = x[e], b = x[e + 4];
+          x[e] = __half2float(__float2half_rn(rope_dot(a, t.c, -b, t.s)));
+          x[e + 4] = __half2float(__float2half_rn(rope_dot(b, t.c, a, t.s)));
+        }
+      }
     }
-    if (lane == 0) {
+    uint32_t par;
+    bool fine;
+    const uint32_t w = kv4_encode(x, par, fine);
+    if (!mine) continue;
+    uint16_t* dst = val ? reinterpret_cast<uint16_t*>(c.vc + (slot >> 1) * kHeadDim) + (slot & 1)
+                        : reinterpret_cast<uint16_t*>(c.kc + slot * (kHeadDim / 2));
+    dst[val ? 4 * u : u] = (uint16_t)w;
+    dst[val ? 4 * u + 2 : u + 16] = (uint16_t)(w >> 16);
+    if (u == 0) {
       reinterpret_cast<uint32_t*>(val ? c.vp : c.kp)[slot] = par;
       if (!fine) atomicOr(&g_kv4_status, SQ_DEV_NONFINITE_KV);
     }
@@ -113,7 +127,11 @@ __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(const __half
 
 cudaError_t launch_kv4_append(const __half* qkv, const Packed& pk, int Hq, int Hkv, double theta,
                               const KV4Cache& c, cudaStream_t st) {
-  return launch_pdl(kv4_append_kernel, dim3((unsigned)((pk.N + kAppendRows - 1) / kAppendRows)), dim3(kAppendThreads), 0,
+  constexpr int kRows = 4;
+  if (pk.N <= device_sm_count())
+    return launch_pdl(kv4_append_kernel<1>, dim3((unsigned)pk.N), dim3(kAppendThreads), 0, st, qkv, pk, Hq, Hkv,
+                      rope_freq(theta), c);
+  return launch_pdl(kv4_append_kernel<kRows>, dim3((unsigned)((pk.N + kRows - 1) / kRows)), dim3(kAppendThreads), 0,
                     st, qkv, pk, Hq, Hkv, rope_freq(theta), c);
 }
 

@@ -10,8 +10,8 @@
 // on the second walk without sorting: the top-th largest of the maxima of
 // groups of threads bounds them from below, and about one entry in a thousand
 // passes.  They are ranked by counting, in each CTA and then in the first.
-// Bound: the logits' bytes from memory for many rows; for one row the three
-// meetings of the cluster.
+// Bound: the logits' bytes from memory for many rows; for one row the cluster's
+// three meetings.
 #include "sq_serve.h"
 
 #include <mutex>
@@ -21,7 +21,7 @@ namespace sq {
 static __device__ unsigned int g_lp_status;
 
 constexpr int kLpThreads = 256, kLpWarps = kLpThreads / 32;
-constexpr int kLpChunk = 20480;    // entries of a CTA, where clusters of 16 allow it
+constexpr int kLpChunk = 25600;    // entries of a CTA, where clusters of 16 allow it
 constexpr int kLpMaxCluster = 16;
 constexpr int kLpList = 512;       // candidates of a CTA
 constexpr int kLpParts = 4;        // copies of a CTA's share, each waited for by itself
@@ -45,6 +45,7 @@ __device__ __forceinline__ uint32_t lp_rank() {
   return r;
 }
 __device__ __forceinline__ void lp_sync(int S) {
+  __syncwarp();
   if (S > 1)
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
   else
@@ -60,10 +61,11 @@ __device__ __forceinline__ uint32_t lp_ld32(const void* local, uint32_t rank) {
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(lp_remote(local, rank)) : "memory");
   return v;
 }
-__device__ __forceinline__ unsigned long long lp_ld64(const void* local, uint32_t rank) {
-  unsigned long long v;
-  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(lp_remote(local, rank)) : "memory");
-  return v;
+__device__ __forceinline__ void lp_st32(const void* local, uint32_t rank, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(lp_remote(local, rank)), "r"(v) : "memory");
+}
+__device__ __forceinline__ void lp_st64(const void* local, uint32_t rank, unsigned long long v) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(lp_remote(local, rank)), "l"(v) : "memory");
 }
 __device__ __forceinline__ float lp_ex2(float x) {
   float y;
@@ -72,14 +74,16 @@ __device__ __forceinline__ float lp_ex2(float x) {
 }
 
 struct LpShared {
-  unsigned long long list[kLpList];              // candidates
-  unsigned long long best[kLogprobsMaxTop];      // this CTA's largest, in order
+  unsigned long long list[kLpList];  // candidates
+  unsigned long long merge[kLpMaxCluster * kLogprobsMaxTop];  // first CTA: every CTA's largest
   uint64_t bar[kLpParts];
-  uint32_t group[32];                            // maxima of this CTA's groups of threads
+  uint4 group4[kLpMaxCluster * 8 / 4];  // maxima of the groups of threads of all CTAs
   uint32_t hist[256];
   float sum[2][kLpWarps];
-  float total[2];
-  unsigned int count, equal, overflow, tau, above;
+  float total[2][kLpMaxCluster];     // first CTA: sums of every CTA
+  unsigned int ones[kLpMaxCluster];
+  unsigned int over[kLpMaxCluster];  // a CTA's list was too short
+  unsigned int count, equal, tau, above;
 };
 
 // Ranks n keys of the list by counting; the first k go to `best`.
@@ -116,7 +120,7 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprobs_kernel(const LogprobAr
   if (tid == 0) {
     for (int p = 0; p < kLpParts; ++p) mbar_init(&s.bar[p], 1);
     fence_mbar_init();
-    s.count = s.equal = s.overflow = 0;
+    s.count = s.equal = 0;
     for (int p = 0; p < kLpParts; ++p) {
       const int b = w0 + (int)((int64_t)(w1 - w0) * p / kLpParts), e = w0 + (int)((int64_t)(w1 - w0) * (p + 1) / kLpParts);
       mbar_arrive_expect_tx(&s.bar[p], (uint32_t)(e - b) * 16);
@@ -129,6 +133,8 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprobs_kernel(const LogprobAr
     if (tid < 8 ? w0 > 0 : w1 < words)
       row[i] = i >= shift && i < shift + n ? src[i - shift] : __ushort_as_half(0xfc00);
   }
+  __syncwarp();
+  if (S > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   __syncthreads();
 
   // ---- first walk: maxima (a NaN stays one)
@@ -149,33 +155,38 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprobs_kernel(const LogprobAr
     for (; part < kLpParts; ++part) late |= !mbar_wait_bounded(&s.bar[part], 0u);
   }
   if (late) atomicOr(&g_lp_status, SQ_DEV_TIMEOUT);
+  // ---- the row's maximum, and the top-th largest of the groups' maxima: every
+  // CTA gets them all (written to it: a read would wait for the way there too)
+  uint32_t* group = reinterpret_cast<uint32_t*>(s.group4);
+  const int total = S * groups;  // 32 to 128
+  __syncwarp();
+  if (S > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // all have begun
   {
     const uint32_t b = *reinterpret_cast<const uint32_t*>(&mx);
     uint32_t o = max(lp_order16(b & 0xffffu), lp_order16(b >> 16));
     const int span = kLpThreads / groups;  // threads of a group: 8, 16 or 32
     for (int i = span >> 1; i > 0; i >>= 1) o = max(o, __shfl_xor_sync(0xffffffffu, o, i));
-    if (tid % span == 0) s.group[tid / span] = o;
+    const uint32_t at = rank * groups + tid / span;
+    o = (o << 8) | (255u - at);  // different keys for equal maxima
+    if (S == 1) {
+      if (tid % span == 0) group[at] = o;
+    } else {
+      for (int i = tid % span; i < S; i += span) lp_st32(&group[at], (uint32_t)i, o);
+    }
   }
   lp_sync(S);
-  // ---- the row's maximum, and the top-th largest of the groups' maxima
-  uint32_t mo;
-  {
-    const int total = S * groups;  // at most 128
-    uint32_t v = 0;
-    if (tid < total) v = S > 1 ? lp_ld32(&s.group[tid % groups], (uint32_t)(tid / groups)) : s.group[tid];
-    __syncthreads();
-    if (tid < total) s.list[tid] = lp_key(v, (uint32_t)tid);  // (the list is not used yet)
-    __syncthreads();
-    if (tid < total) {
-      const unsigned long long key = s.list[tid];
-      int above = 0;
-      for (int j = 0; j < total; ++j) above += s.list[j] > key;
-      if (above == 0) s.above = v;
-      if (above == (top > 0 ? top - 1 : 0)) s.tau = v;
+  if (tid < total) {
+    const uint32_t key = group[tid];
+    int above = 0;
+    for (int j = 0; j < total / 4; ++j) {
+      const uint4 q = s.group4[j];
+      above += (q.x > key) + (q.y > key) + (q.z > key) + (q.w > key);
     }
-    __syncthreads();
-    mo = s.above;
+    if (above == 0) s.above = key >> 8;
+    if (above == (top > 0 ? top - 1 : 0)) s.tau = key >> 8;
   }
+  __syncthreads();
+  const uint32_t mo = s.above;
   const float m = lp_value(mo);
   const bool bad = mo >= 0xfc00u, none = mo == 0x3ffu;  // +inf or NaN; nothing but -inf
   if (bad || none) {
@@ -190,8 +201,7 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprobs_kernel(const LogprobAr
         a.top_logprobs[r * top + tid] = NAN;
       }
     }
-    lp_sync(S);  // (no CTA leaves while another reads its maxima)
-    return;
+    return;  // (nothing more is written to or read from another CTA)
   }
 
   // Candidates of one word: entries above tau, and of those equal to it the
@@ -231,59 +241,100 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprobs_kernel(const LogprobAr
   // ---- second walk: the sums, apart from entries equal to the maximum (their
   // terms are ones, counted: a sure row's logarithm keeps what is left)
   uint32_t tau = s.tau;
-  const float sc = a.invT * 1.4426950408889634f;
-  float S0 = 0.0f, S1 = 0.0f, E0 = 0.0f, E1 = 0.0f;
   unsigned int ones = 0;
-  const __half tau_h = __float2half_rn(lp_value(tau));
-  const __half2 tau2 = __halves2half2(tau_h, tau_h);
-  for (int wb = 0; wb < words; wb += kLpThreads) {
-    const int w = wb + tid;
-    uint4 q = make_uint4(0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u);
-    if (w < words) q = reinterpret_cast<const uint4*>(lp_smem)[w];
-    const __half2* h = reinterpret_cast<const __half2*>(&q);
-    const __half2 wm = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
-    const bool any = w < words && !__hblt2(wm, tau2);  // an entry at tau or above
-    const bool near = any && !__hblt2(wm, __half2half2(__float2half_rn(m)));  // at the maximum
+  {
+    const float sc = a.invT * 1.4426950408889634f;
+    const unsigned long long m2 = f2pack(-m, -m), sc2 = f2pack(sc, sc);
+    unsigned long long Sa = 0, Sb = 0, Ea = 0, Eb = 0;
+    const __half2 tau2 = __half2half2(__float2half_rn(lp_value(tau))), mh2 = __half2half2(__float2half_rn(m));
+    for (int wb = 0; wb < words; wb += kLpThreads) {
+      const int w = wb + tid;
+      uint4 q = make_uint4(0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u);
+      if (w < words) q = reinterpret_cast<const uint4*>(lp_smem)[w];
+      const __half2* h = reinterpret_cast<const __half2*>(&q);
+      const __half2 wm = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+      const bool any = w < words && !__hblt2(wm, tau2);  // an entry at tau or above
+      const bool near = any && !__hblt2(wm, mh2);        // at the maximum
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float2 f = __half22float2(h[e]);
-      // (clamped: -inf has no weight, and 2^-150 is zero)
-      float y0 = fmaxf((f.x - m) * sc, -150.0f), y1 = fmaxf((f.y - m) * sc, -150.0f);
-      float e0 = lp_ex2(y0), e1 = lp_ex2(y1);
-      if (near) {
-        ones += (f.x == m) + (f.y == m);
-        e0 = f.x == m ? 0.0f : e0;
-        e1 = f.y == m ? 0.0f : e1;
+      for (int e = 0; e < 4; ++e) {
+        const float2 f = __half22float2(h[e]);
+        unsigned long long y;
+        asm("add.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(f2pack(f.x, f.y)), "l"(m2));
+        asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(y) : "l"(sc2));
+        float2 x = f2unpack(y);
+        x.x = fmaxf(x.x, -150.0f);  // (-inf: no weight, 2^-150 is zero, and no NaN in the entropy)
+        x.y = fmaxf(x.y, -150.0f);
+        y = f2pack(x.x, x.y);
+        float e0 = lp_ex2(x.x), e1 = lp_ex2(x.y);
+        if (near) {
+          ones += (f.x == m) + (f.y == m);
+          e0 = f.x == m ? 0.0f : e0;
+          e1 = f.y == m ? 0.0f : e1;
+        }
+        const unsigned long long ee = f2pack(e0, e1);
+        if (e & 1) {
+          asm("add.rn.f32x2 %0, %0, %1;" : "+l"(Sb) : "l"(ee));
+          ffma2(Eb, ee, y);
+        } else {
+          asm("add.rn.f32x2 %0, %0, %1;" : "+l"(Sa) : "l"(ee));
+          ffma2(Ea, ee, y);
+        }
       }
-      S0 += e0;
-      S1 += e1;
-      E0 = fmaf(e0, y0, E0);
-      E1 = fmaf(e1, y1, E1);
+      if (top > 0) offer(reinterpret_cast<const uint16_t*>(&q), w, any, tau);
     }
-    if (top > 0) offer(reinterpret_cast<const uint16_t*>(&q), w, any, tau);
-  }
-  S0 = warp_sum(S0 + S1);
-  E0 = warp_sum(E0 + E1);
-  ones = __reduce_add_sync(0xffffffffu, ones);
-  if (lane == 0) {
-    s.sum[0][warp] = S0;
-    s.sum[1][warp] = E0;
-    if (ones) atomicAdd(&s.equal, ones);
+    const float2 s0 = f2unpack(Sa), s1 = f2unpack(Sb), e0 = f2unpack(Ea), e1 = f2unpack(Eb);
+    const float S0 = warp_sum((s0.x + s0.y) + (s1.x + s1.y)), E0 = warp_sum((e0.x + e0.y) + (e1.x + e1.y));
+    ones = __reduce_add_sync(0xffffffffu, ones);
+    if (lane == 0) {
+      s.sum[0][warp] = S0;
+      s.sum[1][warp] = E0;
+      if (ones) atomicAdd(&s.equal, ones);
+    }
   }
   __syncthreads();
+  // results to the first CTA; whether a list was too short to all
   if (tid < 2) {
     float t = 0.0f;
     for (int i = 0; i < kLpWarps; ++i) t += s.sum[tid][i];
-    s.total[tid] = t;
+    if (S > 1)
+      lp_st32(&s.total[tid][rank], 0u, __float_as_uint(t));
+    else
+      s.total[tid][0] = t;
+  } else if (tid == 2) {
+    if (S > 1)
+      lp_st32(&s.ones[rank], 0u, s.equal);
+    else
+      s.ones[0] = s.equal;
+  } else if (tid >= 32 && tid < 32 + S) {
+    const uint32_t o = s.count > kLpList;
+    if (S > 1)
+      lp_st32(&s.over[rank], (uint32_t)(tid - 32), o);
+    else
+      s.over[0] = o;
   }
-  if (tid == 0) s.overflow = s.count > kLpList;
+  // this CTA's `top` largest of its list to the first CTA
+  auto deliver = [&]() {
+    const int have = min((int)s.count, kLpList);
+    for (int i = tid + have; i < top; i += kLpThreads)  // places that stay empty
+      if (S > 1)
+        lp_st64(&s.merge[rank * top + i], 0u, 0ull);
+      else
+        s.merge[i] = 0;
+    lp_ranked(s.list, have, top, [&](int i, unsigned long long key) {
+      if (S > 1)
+        lp_st64(&s.merge[rank * top + i], 0u, key);
+      else
+        s.merge[i] = key;
+    });
+  };
+  if (top > 0) deliver();
   lp_sync(S);
 
   // ---- rarely (rows in order, say) more pass than the list holds: the top-th
   // largest logit itself, by two walks that count its upper and its lower byte
   if (top > 0) {
     bool over = false;
-    for (int i = 0; i < S; ++i) over |= (S > 1 ? lp_ld32(&s.overflow, (uint32_t)i) : s.overflow) != 0;
+    for (int i = 0; i < S; ++i) over |= s.over[i] != 0;
     if (over) {
       uint32_t prefix = 0;
       unsigned int above = 0;  // entries above the bytes found so far
@@ -322,20 +373,17 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprobs_kernel(const LogprobAr
         offer(reinterpret_cast<const uint16_t*>(&q), w, w < words, tau);
       }
       __syncthreads();
+      deliver();
+      lp_sync(S);
     }
-    // this CTA's largest, then the row's
-    if (tid < top) s.best[tid] = 0;
-    __syncthreads();
-    lp_ranked(s.list, min((int)s.count, kLpList), top, [&](int i, unsigned long long key) { s.best[i] = key; });
-    lp_sync(S);
   }
   if (rank == 0) {
     float t0 = 0.0f, t1 = 0.0f;
     unsigned int eq = 0;
     for (int i = 0; i < S; ++i) {
-      t0 += S > 1 ? __uint_as_float(lp_ld32(&s.total[0], (uint32_t)i)) : s.total[0];
-      t1 += S > 1 ? __uint_as_float(lp_ld32(&s.total[1], (uint32_t)i)) : s.total[1];
-      eq += S > 1 ? lp_ld32(&s.equal, (uint32_t)i) : s.equal;
+      t0 += s.total[0][i];
+      t1 += s.total[1][i];
+      eq += s.ones[i];
     }
     const float rest = t0 + (float)(eq - 1);
     const float lse = log1pf(rest);
@@ -348,18 +396,12 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprobs_kernel(const LogprobAr
         a.logprob[r] = ok ? (__half2float(z[t]) - m) * a.invT - lse : NAN;
       }
     }
-    if (top > 0) {
-      const int all = S * top;  // at most kLpList
-      for (int i = tid; i < all; i += kLpThreads)
-        s.list[i] = S > 1 ? lp_ld64(&s.best[i % top], (uint32_t)(i / top)) : s.best[i];
-      __syncthreads();
-      lp_ranked(s.list, all, top, [&](int i, unsigned long long key) {
+    if (top > 0)
+      lp_ranked(s.merge, S * top, top, [&](int i, unsigned long long key) {
         a.top_tokens[r * top + i] = (int32_t)(0xffffffffu - (uint32_t)key);
         a.top_logprobs[r * top + i] = (lp_value((uint32_t)(key >> 32)) - m) * a.invT - lse;
       });
-    }
   }
-  lp_sync(S);  // no CTA leaves while the first reads its results
 }
 
 // CTAs a row: shares of kLpChunk entries; more of them where rows alone leave

@@ -4,6 +4,7 @@
 //   k'_t = fp16(R(pos_t) k_t), cached with v_t at pos_t = pos0 + t
 //   out_t = sum_{j <= pos_t} p_tj v_j / sum_j p_tj,
 //   p_tj = exp(q'_t . k'_j / sqrt(D)), q'_t = fp16(R(pos_t) q_t)
+// (R by rope_dot for what is kept, in plain fp32 for queries).
 //
 // Two launches.  prompt_prepare_kernel rotates and appends, writes the rotated
 // queries where TMA can fetch them, and one of its CTAs lays out the work of
@@ -248,13 +249,18 @@ __global__ void __launch_bounds__(kPrPrepThreads) prompt_prepare_kernel(
   const Packed& pk = a.pk;
   const int G = a.G, Hkv = a.Hkv, tid = threadIdx.x;
   __shared__ RopeCS cs[kPrPrepRows][kHeadDim / 2];
+  __shared__ float2 csq[kPrPrepRows][kHeadDim / 2];  // the heads, for queries
   __shared__ int seq[kPrPrepRows], pos[kPrPrepRows];
   const int64_t row0 = (int64_t)(blockIdx.x - 1) * kPrPrepRows;
   if (packed_rows<kPrPrepRows>(pk, row0, seq, pos, &g_prompt_status)) return;
   {
     const int i = tid / (kHeadDim / 2), d = tid % (kHeadDim / 2);
     // (eight neighbouring dimensions lie 128 bytes apart, so that the lanes of a head read neighbours)
-    if (seq[i] >= 0 && pos[i] >= 0) cs[i][(d & 7) * 8 + (d >> 3)] = rope_cs_pair(pos[i], rf.f[d]);
+    if (seq[i] >= 0 && pos[i] >= 0) {
+      const RopeCS r = rope_cs_pair(pos[i], rf.f[d]);
+      cs[i][(d & 7) * 8 + (d >> 3)] = r;
+      csq[i][(d & 7) * 8 + (d >> 3)] = make_float2(r.c.h, r.s.h);
+    }
   }
   __syncthreads();
   const int64_t width = (int64_t)(Hq + 2 * Hkv) * kHeadDim;
@@ -280,10 +286,16 @@ __global__ void __launch_bounds__(kPrPrepThreads) prompt_prepare_kernel(
     __half* z2 = reinterpret_cast<__half*>(&y2);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const RopeCS c = cs[i][e * 8 + u];
       const float p = __half2float(e1[e]), q = __half2float(e2[e]);
-      z1[e] = __float2half_rn(rope_dot(p, c.c, -q, c.s));
-      z2[e] = __float2half_rn(rope_dot(q, c.c, p, c.s));
+      if (h < Hq) {  // queries: fp32 does (one in 5000 to the other fp16 neighbour)
+        const float2 c = csq[i][e * 8 + u];
+        z1[e] = __float2half_rn(p * c.x - q * c.y);
+        z2[e] = __float2half_rn(q * c.x + p * c.y);
+      } else {
+        const RopeCS c = cs[i][e * 8 + u];
+        z1[e] = __float2half_rn(rope_dot(p, c.c, -q, c.s));
+        z2[e] = __float2half_rn(rope_dot(q, c.c, p, c.s));
+      }
     }
     __half* dst = h < Hq ? qr + (((int64_t)(h / G) * pk.N + row) * G + h % G) * kHeadDim
                          : kc + (((int64_t)b * Hkv + h - Hq) * pk.max_ctx + pos[i]) * kHeadDim;
