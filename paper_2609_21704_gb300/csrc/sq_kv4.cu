@@ -47,14 +47,21 @@ __device__ __forceinline__ uint32_t kv4_encode(const float x[8], uint32_t& par, 
   if (!fine) par = 0x7fff7fffu;  // NaN: everything read from this row is
   if (!fine || s == 0.0f) return 0;
   const float inv = __frcp_rn(s);
+  const float big = 12582912.0f;  // 1.5 2^23: its last bits count ones
   uint32_t w = 0;
+  float open = 0.0f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float d = __fsub_rn(x[e], lo);
-    const float q = d * inv;
-    float c = rintf(q);
-    if (fabsf(fabsf(q - c) - 0.5f) < 1e-5f) c = rintf(__fdiv_rn(d, s));
-    w |= (uint32_t)fminf(c, 15.0f) << (4 * e);
+    const float q = fminf(__fmul_rn(__fsub_rn(x[e], lo), inv), 15.0f);
+    const float r = __fadd_rn(q, big);
+    open = fmaxf(open, fabsf(q - (r - big)));
+    w |= (__float_as_uint(r) & 15u) << (4 * e);
+  }
+  if (open > 0.4999f) {
+    w = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      w |= (uint32_t)fminf(rintf(__fdiv_rn(__fsub_rn(x[e], lo), s)), 15.0f) << (4 * e);
   }
   return w;
 }
@@ -105,8 +112,8 @@ __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(const __half
         for (int e = 0; e < 4; ++e) {
           const RopeCS t = cs[r][e * 16 + u];
           const float a = x[e], b = x[e + 4];
-          x[e] = __half2float(__float2half_rn(rope_dot(a, t.c, -b, t.s)));
-          x[e + 4] = __half2float(__float2half_rn(rope_dot(b, t.c, a, t.s)));
+          x[e] = __half2float(rope_f16(a, t.c, -b, t.s));
+          x[e + 4] = __half2float(rope_f16(b, t.c, a, t.s));
         }
       }
     }
@@ -139,11 +146,14 @@ __device__ __forceinline__ float2 kv4_params(const __half* p, int64_t slot) {
   return __half22float2(reinterpret_cast<const __half2*>(p)[slot]);
 }
 
-// One CTA per 64 positions of a (sequence, head); a thread two neighbouring
-// positions' 16 dimensions of keys and values: 8-byte loads, 16-byte stores.
-constexpr int kUnpackRows = 64;
+// One CTA per 32 positions of a (sequence, head); a thread two neighbouring
+// positions' eight dimensions of keys and values, 16-byte stores side by side.
+constexpr int kUnpackRows = 32;
 __device__ __forceinline__ uint32_t kv4_half2(uint32_t nibbles, float2 p) {
-  const __half2 r = __floats2half2_rn(fmaf((float)(nibbles & 15), p.x, p.y), fmaf((float)((nibbles >> 4) & 15), p.x, p.y));
+  // 2^23 + n, less 2^23
+  const float a = __uint_as_float(0x4b000000u | (nibbles & 15u)) - 8388608.0f;
+  const float b = __uint_as_float(0x4b000000u | ((nibbles >> 4) & 15u)) - 8388608.0f;
+  const __half2 r = __floats2half2_rn(fmaf(a, p.x, p.y), fmaf(b, p.x, p.y));
   return *reinterpret_cast<const uint32_t*>(&r);
 }
 // Eight dimensions from four bytes.
@@ -163,23 +173,20 @@ __global__ void __launch_bounds__(256) kv4_unpack_kernel(const KV4Cache c, int H
     if (threadIdx.x == 0 && blockIdx.x == 0) atomicOr(&g_kv4_status, SQ_DEV_BAD_POSITION);
     return;
   }
-  const int64_t j = (int64_t)blockIdx.x * kUnpackRows + (threadIdx.x >> 3) * 2;
-  const int u = threadIdx.x & 7;  // dimensions 16 u ..
+  const int64_t j = (int64_t)blockIdx.x * kUnpackRows + (threadIdx.x >> 4) * 2;
+  const int u = threadIdx.x & 15;  // dimensions 8 u ..
   if (j + 1 < lo || j >= hi) return;
   const int64_t slot = ((int64_t)b * Hkv + h) * max_ctx + j;
-  const uint4 vw = reinterpret_cast<const uint4*>(c.vc + (slot >> 1) * kHeadDim)[u];
+  // (max_ctx is even: both positions of a pair lie in the cache)
+  const uint2 vw = reinterpret_cast<const uint2*>(c.vc + (slot >> 1) * kHeadDim)[u];
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
     if (j + e < lo || j + e >= hi) continue;
-    const float2 kp = kv4_params(c.kp, slot + e), vp = kv4_params(c.vp, slot + e);
-    const uint2 kw = reinterpret_cast<const uint2*>(c.kc + (slot + e) * (kHeadDim / 2))[u];
-    uint4* kd = reinterpret_cast<uint4*>(k + (slot + e) * kHeadDim) + 2 * u;
-    uint4* vd = reinterpret_cast<uint4*>(v + (slot + e) * kHeadDim) + 2 * u;
-    const uint32_t sel = e ? 0x7632u : 0x5410u;  // the position's two bytes of every four
-    kd[0] = kv4_half8(kw.x, kp);
-    kd[1] = kv4_half8(kw.y, kp);
-    vd[0] = kv4_half8(__byte_perm(vw.x, vw.y, sel), vp);
-    vd[1] = kv4_half8(__byte_perm(vw.z, vw.w, sel), vp);
+    const uint32_t kw = reinterpret_cast<const uint32_t*>(c.kc + (slot + e) * (kHeadDim / 2))[u];
+    // the position's two bytes of every four
+    const uint32_t w = __byte_perm(vw.x, vw.y, e ? 0x7632u : 0x5410u);
+    reinterpret_cast<uint4*>(k + (slot + e) * kHeadDim)[u] = kv4_half8(kw, kv4_params(c.kp, slot + e));
+    reinterpret_cast<uint4*>(v + (slot + e) * kHeadDim)[u] = kv4_half8(w, kv4_params(c.vp, slot + e));
   }
 }
 

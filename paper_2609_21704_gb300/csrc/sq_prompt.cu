@@ -4,7 +4,7 @@
 //   k'_t = fp16(R(pos_t) k_t), cached with v_t at pos_t = pos0 + t
 //   out_t = sum_{j <= pos_t} p_tj v_j / sum_j p_tj,
 //   p_tj = exp(q'_t . k'_j / sqrt(D)), q'_t = fp16(R(pos_t) q_t)
-// (R by rope_dot for what is kept, in plain fp32 for queries).
+// (R by rope_f16 for what is kept, in plain fp32 for queries).
 //
 // Two launches.  prompt_prepare_kernel rotates and appends, writes the rotated
 // queries where TMA can fetch them, and one of its CTAs lays out the work of
@@ -293,8 +293,8 @@ __global__ void __launch_bounds__(kPrPrepThreads) prompt_prepare_kernel(
         z2[e] = __float2half_rn(q * c.x + p * c.y);
       } else {
         const RopeCS c = cs[i][e * 8 + u];
-        z1[e] = __float2half_rn(rope_dot(p, c.c, -q, c.s));
-        z2[e] = __float2half_rn(rope_dot(q, c.c, p, c.s));
+        z1[e] = rope_f16(p, c.c, -q, c.s);
+        z2[e] = rope_f16(q, c.c, p, c.s);
       }
     }
     __half* dst = h < Hq ? qr + (((int64_t)(h / G) * pk.N + row) * G + h % G) * kHeadDim
