@@ -499,7 +499,8 @@ SQ_API sq_status sq_attention_kv4(const void* qkv, int B, int T, int Hq, int Hkv
 
 /* ------------------------------------------------------------------------
  * sq_logprobs: what a program answers beside its tokens, or scores a prompt
- * by.  For each of R rows of fp16 logits z [R, V], x_v = (z_v - max z) / T:
+ * by.  For each of R rows of fp16 logits z [R, V], x_v = (z_v - max z) / T
+ * with T = temperature, finite and at least 1e-30:
  *   logprob[r]  = x_t - log sum_v e^(x_v) of t = tokens[r]  (fp32; tokens
  *                 int32 [R] and logprob both given, or both NULL)
  *   entropy[r]  = -sum_v p_v log p_v in nats  (fp32 [R], or NULL)

@@ -827,8 +827,8 @@ sq_status sq_logprobs(const void* z, int64_t R, int64_t V, float temperature, co
                 (long long)V);
   if (top < 0 || top > kLogprobsMaxTop || top > V)
     return fail(SQ_ERR_SHAPE, "%s: need 0 <= top <= %d and top <= V (top=%d)", who, kLogprobsMaxTop, top);
-  if (!(temperature > 0.0f) || !std::isfinite(temperature) || !std::isfinite(1.0f / temperature))
-    return fail(SQ_ERR_INVALID_ARG, "%s: temperature must be positive and finite, and so its reciprocal", who);
+  if (!(temperature >= 1e-30f) || !std::isfinite(temperature))
+    return fail(SQ_ERR_INVALID_ARG, "%s: temperature must be finite and at least 1e-30", who);
   if (R == 0) return SQ_OK;
   if (!z) return fail(SQ_ERR_INVALID_ARG, "%s: NULL z", who);
   if ((tokens == nullptr) != (logprob == nullptr))

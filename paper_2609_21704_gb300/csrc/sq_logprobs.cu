@@ -4,14 +4,15 @@
 //   x_v = (z_v - max z) / T,  S = sum_v e^x_v
 //   log p_v = x_v - log S,  H = log S - sum_v e^x_v x_v / S
 //
-// A cluster of CTAs takes a row and keeps it in shared memory, so that logits
-// are read from memory once although they are walked twice: for the maximum,
-// then for the sums.  The entries that may be among the `top` largest are found
-// on the second walk without sorting: the top-th largest of the maxima of
-// groups of threads bounds them from below, and about one entry in a thousand
-// passes.  They are ranked by counting, in each CTA and then in the first.
-// Bound: the logits' bytes from memory for many rows; for one row the cluster's
-// three meetings.
+// One reading of the logits: a warp keeps a running maximum and sums relative to
+// it, rescaled in the few steps where it grows.  A CTA takes a row, or a cluster
+// a row where rows are few; its warps' sums and the maxima of groups of threads
+// meet at the end.  Of the entries only those at least the top-th largest of the
+// groups' maxima can be among the `top` largest: threads that met one in a
+// sixteenth of their part read that again (out of L2), and what passes, some tens
+// of entries, is ranked by counting.
+// Bound: the logits' bytes from memory for many rows; for one row the chain of
+// its cluster's three meetings.
 #include "sq_serve.h"
 
 #include <mutex>
@@ -21,10 +22,11 @@ namespace sq {
 static __device__ unsigned int g_lp_status;
 
 constexpr int kLpThreads = 256, kLpWarps = kLpThreads / 32;
-constexpr int kLpChunk = 25600;    // entries of a CTA, where clusters of 16 allow it
+constexpr int kLpPerSm = 4;       // CTAs that share an SM
 constexpr int kLpMaxCluster = 16;
-constexpr int kLpList = 512;       // candidates of a CTA
-constexpr int kLpParts = 4;        // copies of a CTA's share, each waited for by itself
+constexpr int kLpList = 512;      // candidates of a CTA
+constexpr int kLpSegments = 16;   // parts of a thread's words whose maxima are kept
+constexpr int kLpAhead = 4;       // words of a thread in flight
 
 // Total order of (logit, index): largest logit first, lowest index among
 // equals (-0 equals 0).  Larger keys come first; 0 is no entry's key.
@@ -73,18 +75,46 @@ __device__ __forceinline__ float lp_ex2(float x) {
   return y;
 }
 
+// Sums of part of a row relative to its maximum m (a logit's value, at least the
+// lowest finite one): of 2^y and y 2^y over entries below it, y = (z - m) c, and
+// the number of entries equal to it.
+struct LpSums {
+  float m, S, E;
+  unsigned int eq;
+};
+
 struct LpShared {
+  uint4 ring[kLpAhead][kLpThreads];  // a thread's words, its own place each
   unsigned long long list[kLpList];  // candidates
   unsigned long long merge[kLpMaxCluster * kLogprobsMaxTop];  // first CTA: every CTA's largest
-  uint64_t bar[kLpParts];
   uint4 group4[kLpMaxCluster * 8 / 4];  // maxima of the groups of threads of all CTAs
+  uint16_t segment[kLpSegments][kLpThreads];  // maxima (in order) of parts of a thread's words
   uint32_t hist[256];
-  float sum[2][kLpWarps];
-  float total[2][kLpMaxCluster];     // first CTA: sums of every CTA
-  unsigned int ones[kLpMaxCluster];
+  LpSums warp[kLpWarps];
+  LpSums cta[kLpMaxCluster];         // first CTA: of every CTA
   unsigned int over[kLpMaxCluster];  // a CTA's list was too short
-  unsigned int count, equal, tau, above;
+  unsigned int count, tau, above, equal;
 };
+
+// Joins b's sums to a's; c = log2(e) / T.
+__device__ __forceinline__ void lp_join(LpSums& a, const LpSums& b, float c) {
+  const float m = fmaxf(a.m, b.m);
+  const float da = (a.m - m) * c, db = (b.m - m) * c;
+  const float fa = lp_ex2(da), fb = lp_ex2(db);
+  // entries equal to the lower maximum become ordinary ones
+  const float Sa = a.S + (a.m < m ? (float)a.eq : 0.0f), Sb = b.S + (b.m < m ? (float)b.eq : 0.0f);
+  a.E = (fa > 0.0f ? fa * fmaf(da, Sa, a.E) : 0.0f) + (fb > 0.0f ? fb * fmaf(db, Sb, b.E) : 0.0f);
+  a.S = fmaf(fa, Sa, fb * Sb);
+  a.eq = (a.m < m ? 0u : a.eq) + (b.m < m ? 0u : b.eq);
+  a.m = m;
+}
+
+__device__ __forceinline__ uint32_t lp_word_max(const uint4& q) {
+  const __half2* h = reinterpret_cast<const __half2*>(&q);
+  const __half2 m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
+  const uint32_t b = *reinterpret_cast<const uint32_t*>(&m);
+  return max(lp_order16(b & 0xffffu), lp_order16(b >> 16));
+}
 
 // Ranks n keys of the list by counting; the first k go to `best`.
 template <typename Emit>
@@ -97,73 +127,161 @@ __device__ __forceinline__ void lp_ranked(const unsigned long long* list, int n,
   }
 }
 
-// S CTAs (a cluster) a row; dynamic shared memory: the share of the row, at
-// the same place within 16 bytes as in memory.
-__global__ void __launch_bounds__(kLpThreads, 4) logprobs_kernel(const LogprobArgs a, int S, int groups) {
+// S CTAs (a cluster) a row.
+__global__ void __launch_bounds__(kLpThreads, kLpPerSm) logprobs_kernel(const LogprobArgs a, int S, int groups) {
   griddep_wait();
   griddep_launch_dependents();
-  extern __shared__ __align__(128) uint8_t lp_smem[];
   __shared__ LpShared s;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t rank = S > 1 ? lp_rank() : 0u;
   const int64_t r = blockIdx.x / (unsigned)S;
   const int64_t c0 = a.V * rank / S, c1 = a.V * (rank + 1) / S;
   const int n = (int)(c1 - c0), top = a.top;
-  const __half* z = a.z + r * a.V;
-  const __half* src = z + c0;
-  const int shift = (int)((reinterpret_cast<uintptr_t>(src) & 15) >> 1);  // entries before ours in the first 16 bytes
-  const int words = (n + shift + 7) / 8;
-  __half* row = reinterpret_cast<__half*>(lp_smem);  // entry i of the share at row[shift + i]
-
-  // ---- the share: whole 16-byte pieces by bulk copies, ragged ends by hand
-  const int w0 = shift ? 1 : 0, w1 = max((n + shift) / 8, w0);  // whole words
-  if (tid == 0) {
-    for (int p = 0; p < kLpParts; ++p) mbar_init(&s.bar[p], 1);
-    fence_mbar_init();
-    s.count = s.equal = 0;
-    for (int p = 0; p < kLpParts; ++p) {
-      const int b = w0 + (int)((int64_t)(w1 - w0) * p / kLpParts), e = w0 + (int)((int64_t)(w1 - w0) * (p + 1) / kLpParts);
-      mbar_arrive_expect_tx(&s.bar[p], (uint32_t)(e - b) * 16);
-      if (e > b) bulk_g2s(lp_smem + b * 16, src - shift + b * 8, (uint32_t)(e - b) * 16, &s.bar[p]);
-    }
-  }
-  // ends, and what pads the first and the last word: -inf
-  if (tid < 16) {
-    const int i = tid < 8 ? tid : w1 * 8 + tid - 8;  // place in shared memory
-    if (tid < 8 ? w0 > 0 : w1 < words)
-      row[i] = i >= shift && i < shift + n ? src[i - shift] : __ushort_as_half(0xfc00);
-  }
+  if (tid == 0) s.count = 0;
   __syncwarp();
   if (S > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  __syncthreads();
+  // this share in words of eight entries at 16-byte borders; entry i of the
+  // share is entry shift + i of the words, and step i of this thread its word
+  // i * kLpThreads + tid
+  const __half* src = a.z + r * a.V + c0;
+  const int shift = (int)((reinterpret_cast<uintptr_t>(src) & 15) >> 1);
+  const uint4* data = reinterpret_cast<const uint4*>(src - shift);
+  const int words = (n + shift + 7) / 8, steps = (words + kLpThreads - 1) / kLpThreads;
+  const int per_segment = (steps + kLpSegments - 1) / kLpSegments;
+  // this warp's steps of whole words only: plain0 <= i < plain1
+  const int plain0 = shift > 0 && warp == 0 ? 1 : 0;
+  const int plain1 = ((n + shift) / 8 - warp * 32 - 32 + kLpThreads) / kLpThreads;
+  auto whole = [&](int w) { return w * 8 >= shift && w * 8 + 8 <= n + shift; };
+  // a word; at the ends entry by entry, -inf for what is not in the share
+  auto load = [&](int w) {
+    if (whole(w)) return __ldg(data + w);
+    uint4 q = make_uint4(0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u);
+    uint16_t* h = reinterpret_cast<uint16_t*>(&q);
+    if (w < words)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (w * 8 + i >= shift && w * 8 + i < n + shift) h[i] = __half_as_ushort(src[w * 8 + i - shift]);
+    return q;
+  };
 
-  // ---- first walk: maxima (a NaN stays one)
-  __half2 mx = __halves2half2(__ushort_as_half(0xfc00), __ushort_as_half(0xfc00));
-  bool late = false;
-  {
-    int part = 0;
-    for (int w = tid; w < words; w += kLpThreads) {
-      // every part up to the one that holds this word
-      while (part < kLpParts && w >= w0 + (int)((int64_t)(w1 - w0) * part / kLpParts)) {
-        late |= !mbar_wait_bounded(&s.bar[part], 0u);
-        ++part;
-      }
-      const uint4 q = reinterpret_cast<const uint4*>(lp_smem)[w];
+  // ---- the walk.  y = z c + b, b = -m c rounded once for the warp's maximum m
+  // (what that is off by is put right at the end); entries equal to m are counted
+  // and left out of the sums, so that what lies beside a sure token is kept.  An
+  // entry of -inf makes the second sum NaN (0 x -inf): the warp then walks again
+  // with y cut off at -150, where 2^y is zero.
+  const float c = a.invT * 1.4426950408889634f;
+  uint32_t mine = 0;  // this thread's maximum, in order
+  LpSums sum;
+#pragma unroll 1
+  for (int cut = 0; cut < 2; ++cut) {
+    unsigned long long Sa = 0, Sb = 0, Ea = 0, Eb = 0;
+    const unsigned long long c2 = f2pack(c, c);
+    uint32_t mo = lp_order16(0xfbffu), seg = 0;
+    __half2 mh2 = __half2half2(__ushort_as_half(0xfbff));
+    __half2 mx = __half2half2(__ushort_as_half(0xfc00));
+    float m = -65504.0f, b = 65504.0f * c;
+    unsigned int eq = 0;
+    const uint32_t ring = smem_u32(&s.ring[0][tid]);
+    auto request = [&](int i) {
+      if (i >= plain0 && i < plain1)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(
+                         ring + (uint32_t)(i % kLpAhead) * (uint32_t)(kLpThreads * 16)),
+                     "l"(data + i * kLpThreads + tid)
+                     : "memory");
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int i = 0; i < kLpAhead - 1; ++i) request(i);
+    int left = per_segment;
+#pragma unroll 1
+    for (int i = 0; i < steps; ++i) {
+      request(i + kLpAhead - 1);
+      asm volatile("cp.async.wait_group %0;" ::"n"(kLpAhead - 1) : "memory");
+      const bool plain = i >= plain0 && i < plain1;
+      uint4 q = s.ring[i % kLpAhead][tid];
+      if (!plain) q = load(i * kLpThreads + tid);
       const __half2* h = reinterpret_cast<const __half2*>(&q);
-      mx = __hmax2_nan(__hmax2_nan(mx, __hmax2_nan(h[0], h[1])), __hmax2_nan(h[2], h[3]));
+      const __half2 wm = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
+      mx = __hmax2_nan(mx, wm);
+      const bool grown = !__hblt2(wm, mh2);  // (a NaN is not less either)
+      const unsigned long long b2 = f2pack(b, b);
+      float y[8], e[8];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 x = __half22float2(h[k]);
+        unsigned long long yy;
+        asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(yy) : "l"(f2pack(x.x, x.y)), "l"(c2), "l"(b2));
+        const float2 v = f2unpack(yy);
+        y[2 * k] = v.x;
+        y[2 * k + 1] = v.y;
+        e[2 * k] = lp_ex2(v.x);
+        e[2 * k + 1] = lp_ex2(v.y);
+      }
+      if (__any_sync(0xffffffffu, grown) || !plain || cut) {
+        const uint32_t o = __reduce_max_sync(0xffffffffu, lp_word_max(q));
+        if (o > mo) {  // a larger maximum: the sums relative to it
+          mo = o;
+          const float m1 = lp_value(o), b1 = __fmul_rn(-m1, c), d = b1 - b, f = lp_ex2(d);
+          const float2 s0 = f2unpack(Sa), s1 = f2unpack(Sb), e0 = f2unpack(Ea), e1 = f2unpack(Eb);
+          const float S0 = (s0.x + s0.y) + (s1.x + s1.y) + (float)eq, E0 = (e0.x + e0.y) + (e1.x + e1.y);
+          Sa = f2pack(f * S0, 0.0f);
+          Ea = f2pack(f > 0.0f ? f * fmaf(d, S0, E0) : 0.0f, 0.0f);
+          Sb = Eb = 0;
+          eq = 0;
+          m = m1;
+          b = b1;
+          mh2 = __half2half2(__float2half_rn(m1));
+        }
+        const uint16_t* z = reinterpret_cast<const uint16_t*>(&q);
+        const int w = i * kLpThreads + tid;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const bool in = w * 8 + k >= shift && w * 8 + k < n + shift;
+          const bool one = in && lp_order16(z[k]) == mo;
+          eq += one;
+          float v = fmaf(__half2float(__ushort_as_half(z[k])), c, b);
+          if (cut || !in) v = fmaxf(v, -150.0f);
+          y[k] = v;
+          e[k] = one || !in ? 0.0f : lp_ex2(v);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; k += 2) {
+        const unsigned long long ea = f2pack(e[2 * k], e[2 * k + 1]), eb = f2pack(e[2 * k + 2], e[2 * k + 3]);
+        asm("add.rn.f32x2 %0, %0, %1;" : "+l"(Sa) : "l"(ea));
+        asm("add.rn.f32x2 %0, %0, %1;" : "+l"(Sb) : "l"(eb));
+        ffma2(Ea, ea, f2pack(y[2 * k], y[2 * k + 1]));
+        ffma2(Eb, eb, f2pack(y[2 * k + 2], y[2 * k + 3]));
+      }
+      if (--left == 0 || i == steps - 1) {
+        const uint32_t bits = *reinterpret_cast<const uint32_t*>(&mx);
+        const uint32_t o = max(lp_order16(bits & 0xffffu), lp_order16(bits >> 16));
+        s.segment[seg++][tid] = (uint16_t)o;
+        mine = max(mine, o);
+        mx = __half2half2(__ushort_as_half(0xfc00));
+        left = per_segment;
+      }
     }
-    for (; part < kLpParts; ++part) late |= !mbar_wait_bounded(&s.bar[part], 0u);
+    const float2 s0 = f2unpack(Sa), s1 = f2unpack(Sb), e0 = f2unpack(Ea), e1 = f2unpack(Eb);
+    sum.m = m;
+    sum.S = warp_sum((s0.x + s0.y) + (s1.x + s1.y));
+    sum.E = warp_sum((e0.x + e0.y) + (e1.x + e1.y));
+    sum.eq = __reduce_add_sync(0xffffffffu, eq);
+    // y is `skew` less than (z - m) c
+    const float skew = fmaf(-m, c, -b), f = lp_ex2(skew);
+    sum.E = f * fmaf(skew, sum.S, sum.E);
+    sum.S *= f;
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    if (!isnan(sum.E)) break;  // (the whole warp)
   }
-  if (late) atomicOr(&g_lp_status, SQ_DEV_TIMEOUT);
-  // ---- the row's maximum, and the top-th largest of the groups' maxima: every
-  // CTA gets them all (written to it: a read would wait for the way there too)
+
+  // ---- the groups' maxima to every CTA of the row, sums to the first
   uint32_t* group = reinterpret_cast<uint32_t*>(s.group4);
   const int total = S * groups;  // 32 to 128
   __syncwarp();
   if (S > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // all have begun
   {
-    const uint32_t b = *reinterpret_cast<const uint32_t*>(&mx);
-    uint32_t o = max(lp_order16(b & 0xffffu), lp_order16(b >> 16));
+    uint32_t o = mine;
     const int span = kLpThreads / groups;  // threads of a group: 8, 16 or 32
     for (int i = span >> 1; i > 0; i >>= 1) o = max(o, __shfl_xor_sync(0xffffffffu, o, i));
     const uint32_t at = rank * groups + tid / span;
@@ -174,10 +292,36 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprobs_kernel(const LogprobAr
       for (int i = tid % span; i < S; i += span) lp_st32(&group[at], (uint32_t)i, o);
     }
   }
+  if (lane == 0) s.warp[warp] = sum;
+  __syncthreads();
+  if (warp == 0) {
+    // lanes 0 .. 7 a warp's sums each, joined in pairs
+    LpSums t = s.warp[lane & 7];
+#pragma unroll
+    for (int i = 4; i > 0; i >>= 1) {
+      LpSums u;
+      u.m = __shfl_down_sync(0xffffffffu, t.m, i);
+      u.S = __shfl_down_sync(0xffffffffu, t.S, i);
+      u.E = __shfl_down_sync(0xffffffffu, t.E, i);
+      u.eq = __shfl_down_sync(0xffffffffu, t.eq, i);
+      lp_join(t, u, c);
+    }
+    if (lane == 0) {
+      if (S > 1) {
+        lp_st32(&s.cta[rank].m, 0u, __float_as_uint(t.m));
+        lp_st32(&s.cta[rank].S, 0u, __float_as_uint(t.S));
+        lp_st32(&s.cta[rank].E, 0u, __float_as_uint(t.E));
+        lp_st32(&s.cta[rank].eq, 0u, t.eq);
+      } else {
+        s.cta[0] = t;
+      }
+    }
+  }
   lp_sync(S);
   if (tid < total) {
     const uint32_t key = group[tid];
     int above = 0;
+#pragma unroll 4
     for (int j = 0; j < total / 4; ++j) {
       const uint4 q = s.group4[j];
       above += (q.x > key) + (q.y > key) + (q.z > key) + (q.w > key);
@@ -204,196 +348,158 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprobs_kernel(const LogprobAr
     return;  // (nothing more is written to or read from another CTA)
   }
 
-  // Candidates of one word: entries above tau, and of those equal to it the
-  // first `top` of a warp, whose words come in rising order.
-  unsigned int ties = 0;  // this warp's
-  auto offer = [&](const uint16_t* h, int w, bool any, uint32_t tau) {
-    if (!__any_sync(0xffffffffu, any)) return;
-    unsigned int mine = 0, hits = 0;
-    uint32_t o[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int i = w * 8 + e - shift;
-      o[e] = any && i >= 0 && i < n ? lp_order16(h[e]) : 0u;
-      mine += o[e] == tau;
-      hits |= (o[e] > tau ? 1u : 0u) << e;
-    }
-    unsigned int before = mine;  // ties of lower lanes
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const unsigned int v = __shfl_up_sync(0xffffffffu, before, d);
-      if (lane >= d) before += v;
-    }
-    const unsigned int all = __shfl_sync(0xffffffffu, before, 31);
-    before -= mine;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      bool take = (hits >> e) & 1;
-      if (o[e] == tau && o[e]) take = ties + before++ < (unsigned)top;
-      if (take) {
-        const unsigned int at = atomicAdd(&s.count, 1u);
-        if (at < kLpList) s.list[at] = lp_key(o[e], (uint32_t)(c0 + w * 8 + e - shift));
-      }
-    }
-    ties += all;
-  };
-
-  // ---- second walk: the sums, apart from entries equal to the maximum (their
-  // terms are ones, counted: a sure row's logarithm keeps what is left)
-  uint32_t tau = s.tau;
-  unsigned int ones = 0;
-  {
-    const float sc = a.invT * 1.4426950408889634f;
-    const unsigned long long m2 = f2pack(-m, -m), sc2 = f2pack(sc, sc);
-    unsigned long long Sa = 0, Sb = 0, Ea = 0, Eb = 0;
-    const __half2 tau2 = __half2half2(__float2half_rn(lp_value(tau))), mh2 = __half2half2(__float2half_rn(m));
-    for (int wb = 0; wb < words; wb += kLpThreads) {
-      const int w = wb + tid;
-      uint4 q = make_uint4(0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u);
-      if (w < words) q = reinterpret_cast<const uint4*>(lp_smem)[w];
-      const __half2* h = reinterpret_cast<const __half2*>(&q);
-      const __half2 wm = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
-      const bool any = w < words && !__hblt2(wm, tau2);  // an entry at tau or above
-      const bool near = any && !__hblt2(wm, mh2);        // at the maximum
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float2 f = __half22float2(h[e]);
-        unsigned long long y;
-        asm("add.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(f2pack(f.x, f.y)), "l"(m2));
-        asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(y) : "l"(sc2));
-        float2 x = f2unpack(y);
-        x.x = fmaxf(x.x, -150.0f);  // (-inf: no weight, 2^-150 is zero, and no NaN in the entropy)
-        x.y = fmaxf(x.y, -150.0f);
-        y = f2pack(x.x, x.y);
-        float e0 = lp_ex2(x.x), e1 = lp_ex2(x.y);
-        if (near) {
-          ones += (f.x == m) + (f.y == m);
-          e0 = f.x == m ? 0.0f : e0;
-          e1 = f.y == m ? 0.0f : e1;
-        }
-        const unsigned long long ee = f2pack(e0, e1);
-        if (e & 1) {
-          asm("add.rn.f32x2 %0, %0, %1;" : "+l"(Sb) : "l"(ee));
-          ffma2(Eb, ee, y);
-        } else {
-          asm("add.rn.f32x2 %0, %0, %1;" : "+l"(Sa) : "l"(ee));
-          ffma2(Ea, ee, y);
-        }
-      }
-      if (top > 0) offer(reinterpret_cast<const uint16_t*>(&q), w, any, tau);
-    }
-    const float2 s0 = f2unpack(Sa), s1 = f2unpack(Sb), e0 = f2unpack(Ea), e1 = f2unpack(Eb);
-    const float S0 = warp_sum((s0.x + s0.y) + (s1.x + s1.y)), E0 = warp_sum((e0.x + e0.y) + (e1.x + e1.y));
-    ones = __reduce_add_sync(0xffffffffu, ones);
-    if (lane == 0) {
-      s.sum[0][warp] = S0;
-      s.sum[1][warp] = E0;
-      if (ones) atomicAdd(&s.equal, ones);
-    }
+  // the given token's logit, on its way while candidates are collected
+  const bool answers = rank == 0 && tid == 0;
+  float zt = 0.0f;
+  bool token_ok = false;
+  if (answers && a.tokens) {
+    const int64_t t = a.tokens[r];
+    token_ok = t >= 0 && t < a.V;
+    if (token_ok) zt = __half2float(a.z[r * a.V + t]);
   }
-  __syncthreads();
-  // results to the first CTA; whether a list was too short to all
-  if (tid < 2) {
-    float t = 0.0f;
-    for (int i = 0; i < kLpWarps; ++i) t += s.sum[tid][i];
-    if (S > 1)
-      lp_st32(&s.total[tid][rank], 0u, __float_as_uint(t));
-    else
-      s.total[tid][0] = t;
-  } else if (tid == 2) {
-    if (S > 1)
-      lp_st32(&s.ones[rank], 0u, s.equal);
-    else
-      s.ones[0] = s.equal;
-  } else if (tid >= 32 && tid < 32 + S) {
-    const uint32_t o = s.count > kLpList;
-    if (S > 1)
-      lp_st32(&s.over[rank], (uint32_t)(tid - 32), o);
-    else
-      s.over[0] = o;
-  }
-  // this CTA's `top` largest of its list to the first CTA
-  auto deliver = [&]() {
-    const int have = min((int)s.count, kLpList);
-    for (int i = tid + have; i < top; i += kLpThreads)  // places that stay empty
-      if (S > 1)
-        lp_st64(&s.merge[rank * top + i], 0u, 0ull);
-      else
-        s.merge[i] = 0;
-    lp_ranked(s.list, have, top, [&](int i, unsigned long long key) {
-      if (S > 1)
-        lp_st64(&s.merge[rank * top + i], 0u, key);
-      else
-        s.merge[i] = key;
-    });
-  };
-  if (top > 0) deliver();
-  lp_sync(S);
-
-  // ---- rarely (rows in order, say) more pass than the list holds: the top-th
-  // largest logit itself, by two walks that count its upper and its lower byte
   if (top > 0) {
-    bool over = false;
-    for (int i = 0; i < S; ++i) over |= s.over[i] != 0;
-    if (over) {
+    uint32_t tau = s.tau;
+    unsigned int ties = 0;  // this warp's entries equal to tau so far
+    // Candidates: entries above tau, and of those equal to it the first `top` of
+    // a warp, whose words are taken in rising order.
+    auto collect = [&]() {
+      const int segments = (steps + per_segment - 1) / per_segment;
+#pragma unroll 1
+      for (int g = 0; g < segments; ++g) {
+        const bool look = s.segment[g][tid] >= tau;
+        if (!__any_sync(0xffffffffu, look)) continue;
+        const int i1 = min((g + 1) * per_segment, steps);
+#pragma unroll 1
+        for (int i0 = g * per_segment; i0 < i1; i0 += 4) {
+          uint4 qs[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            qs[k] = make_uint4(0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u);
+            if (look && i0 + k < i1) qs[k] = load((i0 + k) * kLpThreads + tid);
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int w = (i0 + k) * kLpThreads + tid;
+            const bool any = look && i0 + k < i1 && lp_word_max(qs[k]) >= tau;
+            if (!__any_sync(0xffffffffu, any)) continue;
+            const uint16_t* z = reinterpret_cast<const uint16_t*>(&qs[k]);
+            uint32_t here = 0;  // bits: ties, and above them entries over tau
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const uint32_t o = lp_order16(z[e]);
+              const bool in = any && w * 8 + e >= shift && w * 8 + e < n + shift;
+              here |= (in && o == tau ? 1u : 0u) << e | (in && o > tau ? 256u : 0u) << e;
+            }
+            unsigned int before = __popc(here & 255u);  // ties of lower lanes
+            const unsigned int own = before;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+              const unsigned int v = __shfl_up_sync(0xffffffffu, before, d);
+              if (lane >= d) before += v;
+            }
+            const unsigned int all = __shfl_sync(0xffffffffu, before, 31);
+            before += ties - own;
+#pragma unroll 1
+            for (int e = 0; e < 8; ++e) {
+              bool take = (here >> (8 + e)) & 1u;
+              if ((here >> e) & 1u) take = before++ < (unsigned)top;
+              if (take) {
+                const unsigned int at = atomicAdd(&s.count, 1u);
+                const int64_t v = w * 8 + e - shift;
+                if (at < kLpList)
+                  s.list[at] = lp_key(lp_order16(__half_as_ushort(src[v])), (uint32_t)(c0 + v));
+              }
+            }
+            ties += all;
+          }
+        }
+      }
+    };
+    // this CTA's `top` largest of its list to the first CTA
+    auto deliver = [&]() {
+      const int have = min((int)s.count, kLpList);
+      for (int i = tid + have; i < top; i += kLpThreads)  // places that stay empty
+        if (S > 1)
+          lp_st64(&s.merge[rank * top + i], 0u, 0ull);
+        else
+          s.merge[i] = 0;
+      lp_ranked(s.list, have, top, [&](int i, unsigned long long key) {
+        if (S > 1)
+          lp_st64(&s.merge[rank * top + i], 0u, key);
+        else
+          s.merge[i] = key;
+      });
+    };
+#pragma unroll 1
+    for (int again = 0; again < 2; ++again) {
+      collect();
+      __syncthreads();
+      if (tid < S) {
+        const uint32_t o = s.count > kLpList;
+        if (S > 1)
+          lp_st32(&s.over[rank], (uint32_t)tid, o);
+        else
+          s.over[0] = o;
+      }
+      deliver();
+      lp_sync(S);
+      bool over = false;
+      for (int i = 0; i < S; ++i) over |= s.over[i] != 0;
+      if (!over || again) break;
+      // Rarely (rows in order, say) more pass than the list holds.  Then tau
+      // becomes the top-th largest logit itself, by two walks that count its
+      // upper and its lower byte.
       uint32_t prefix = 0;
       unsigned int above = 0;  // entries above the bytes found so far
+#pragma unroll 1
       for (int byte = 1; byte >= 0; --byte) {
         lp_sync(S);  // (the others have read the last counts)
         s.hist[tid] = 0;
         __syncthreads();
-        for (int i = tid; i < n; i += kLpThreads) {
-          const uint32_t o = lp_order16(__half_as_ushort(row[shift + i]));
-          if (byte == 1 || (o >> 8) == prefix) atomicAdd(&s.hist[byte == 1 ? o >> 8 : o & 255u], 1u);
+#pragma unroll 1
+        for (int w = tid; w < words; w += kLpThreads) {
+          const uint4 q = load(w);
+          const uint16_t* z = reinterpret_cast<const uint16_t*>(&q);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const uint32_t o = lp_order16(z[e]);
+            if (w * 8 + e >= shift && w * 8 + e < n + shift && (byte == 1 || (o >> 8) == prefix))
+              atomicAdd(&s.hist[byte == 1 ? o >> 8 : o & 255u], 1u);
+          }
         }
         lp_sync(S);
-        unsigned int c = 0;
-        for (int i = 0; i < S; ++i) c += S > 1 ? lp_ld32(&s.hist[tid], (uint32_t)i) : s.hist[tid];
+        unsigned int cnt = 0;
+        for (int i = 0; i < S; ++i) cnt += S > 1 ? lp_ld32(&s.hist[tid], (uint32_t)i) : s.hist[tid];
         __syncthreads();
-        s.list[tid] = c;
+        s.list[tid] = cnt;
         __syncthreads();
         unsigned int over_me = above;
         for (int j = tid + 1; j < 256; ++j) over_me += (unsigned int)s.list[j];
-        if (over_me < (unsigned)top && over_me + c >= (unsigned)top) {
+        if (over_me < (unsigned)top && over_me + cnt >= (unsigned)top) {
           s.tau = byte == 1 ? (uint32_t)tid : (prefix << 8) | (uint32_t)tid;
-          s.above = over_me;
+          s.equal = over_me;
         }
         __syncthreads();
         prefix = s.tau;
-        above = s.above;
+        above = s.equal;
       }
       tau = prefix;
+      __syncthreads();
       if (tid == 0) s.count = 0;
       ties = 0;
       __syncthreads();
-      for (int wb = 0; wb < words; wb += kLpThreads) {
-        const int w = wb + tid;
-        uint4 q = make_uint4(0, 0, 0, 0);
-        if (w < words) q = reinterpret_cast<const uint4*>(lp_smem)[w];
-        offer(reinterpret_cast<const uint16_t*>(&q), w, w < words, tau);
-      }
-      __syncthreads();
-      deliver();
-      lp_sync(S);
     }
   }
   if (rank == 0) {
-    float t0 = 0.0f, t1 = 0.0f;
-    unsigned int eq = 0;
-    for (int i = 0; i < S; ++i) {
-      t0 += s.total[0][i];
-      t1 += s.total[1][i];
-      eq += s.ones[i];
-    }
-    const float rest = t0 + (float)(eq - 1);
+    LpSums t = s.cta[0];
+    for (int i = 1; i < S; ++i) lp_join(t, s.cta[i], c);
+    const float rest = t.S + (float)(t.eq - 1);
     const float lse = log1pf(rest);
-    if (tid == 0) {
-      if (a.entropy) a.entropy[r] = lse - t1 * 0.6931471805599453f / (1.0f + rest);
+    if (answers) {
+      if (a.entropy) a.entropy[r] = lse - t.E * 0.6931471805599453f / (1.0f + rest);
       if (a.tokens) {
-        const int64_t t = a.tokens[r];
-        const bool ok = t >= 0 && t < a.V;
-        if (!ok) atomicOr(&g_lp_status, SQ_DEV_BAD_TOKEN_ID);
-        a.logprob[r] = ok ? (__half2float(z[t]) - m) * a.invT - lse : NAN;
+        if (!token_ok) atomicOr(&g_lp_status, SQ_DEV_BAD_TOKEN_ID);
+        a.logprob[r] = token_ok ? (zt - m) * a.invT - lse : NAN;
       }
     }
     if (top > 0)
@@ -404,12 +510,11 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprobs_kernel(const LogprobAr
   }
 }
 
-// CTAs a row: shares of kLpChunk entries; more of them where rows alone leave
-// SMs idle, down to shares of 4096.
+// CTAs a row: one, or as many as fill the SMs (up to 16, in shares of 4096
+// entries at least) where rows are few.
 cudaError_t launch_logprobs(const LogprobArgs& a, cudaStream_t st) {
   static std::mutex mu;
   static bool ready[64] = {false};
-  constexpr int kMaxSmem = 2 * ((1 << 20) / kLpMaxCluster + 16);
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
@@ -417,20 +522,18 @@ cudaError_t launch_logprobs(const LogprobArgs& a, cudaStream_t st) {
   {
     std::lock_guard<std::mutex> lock(mu);
     if (!ready[dev]) {
-      e = cudaFuncSetAttribute(logprobs_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
-      if (e == cudaSuccess) e = cudaFuncSetAttribute(logprobs_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+      e = cudaFuncSetAttribute(logprobs_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
       if (e != cudaSuccess) return e;
       ready[dev] = true;
     }
   }
-  int64_t S = (a.V + kLpChunk - 1) / kLpChunk;
+  int64_t S = (int64_t)kLpPerSm * device_sm_count() / 2 / a.R;
+  if (S > a.V / 4096) S = a.V / 4096;
   if (S > kLpMaxCluster) S = kLpMaxCluster;
-  while (2 * S <= kLpMaxCluster && 2 * S * a.R <= device_sm_count() && a.V / (2 * S) >= 4096) S *= 2;
-  const int64_t share = (a.V + S - 1) / S;
+  if (S < 1) S = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(a.R * S));
   cfg.blockDim = dim3(kLpThreads);
-  cfg.dynamicSmemBytes = (size_t)((share + 15) / 8 * 16);
   cfg.stream = st;
   cudaLaunchAttribute at[2];
   int na = 0;
