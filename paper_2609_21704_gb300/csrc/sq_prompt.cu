@@ -23,7 +23,7 @@ static __device__ unsigned int g_prompt_status;
 constexpr int kPrRows = 256;    // query rows of a work item: two MMA tiles
 constexpr int kPrKeys = 128;    // keys of a block
 constexpr int kPrTile = kPrKeys * kHeadDim * 2;  // bytes of a block's keys (or values)
-constexpr int kPrStages = 5;    // K and V tiles in flight, in turn (odd)
+constexpr int kPrK = 2, kPrV = 3;  // tiles of keys and of values in shared memory
 constexpr int kPrPrepRows = 4;  // rows of a preparing CTA
 constexpr int kPrPrepThreads = 256;
 constexpr int kPrMaxBlocks = (int)(kPromptMaxCtx / kPrKeys);
@@ -374,7 +374,16 @@ __device__ __forceinline__ void tm_st32(uint32_t addr, const uint32_t* r) {
       "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr)
       : "memory");
 }
+// Waits for this thread's TMEM loads.  tm_loaded32: 32 registers that were
+// loaded before the last wait (so that nothing that reads them moves above it).
 __device__ __forceinline__ void tm_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tm_loaded32(uint32_t* r) {
+#pragma unroll
+  for (int i = 0; i < 32; i += 8)
+    asm volatile(""
+                 : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]),
+                   "+r"(r[i + 6]), "+r"(r[i + 7]));
+}
 __device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ unsigned long long ffma2_to(unsigned long long a, unsigned long long b,
@@ -414,25 +423,37 @@ constexpr float kPrBias = 10.0f, kPrSlack = 5.0f;
 
 constexpr int kPrThreads = 384;
 constexpr int kPrOffKV = 2 * kPrTile;  // behind the queries
-constexpr int kPrOffBar = kPrOffKV + kPrStages * kPrTile;
+constexpr int kPrOffBar = kPrOffKV + (kPrK + kPrV) * kPrTile;
 constexpr int kPrSmem = kPrOffBar + 512 + 1024;  // and room to align the tiles to 1024 bytes
 
 struct PromptBars {
-  uint64_t q_full, q_empty, kv_full[kPrStages], kv_empty[kPrStages], v_ready[kPrStages], s_full[2], p_ready[2],
-      o_done[2], drain;
+  uint64_t q_full, q_empty, k_full[kPrK], k_empty[kPrK], v_full[kPrV], v_empty[kPrV], v_ready[kPrV], s_full[2],
+      p_ready[2][2], o_done[2], drain;
   uint32_t tmem;
   int dead;     // a wait has run out: no one waits any more
   int odd[8];   // [round % 8]: 1 + the round in which a value that is not finite was met (the
-                // values' warps are at most three rounds ahead: kPrStages tiles)
+                // values' warps are at most kPrV blocks ahead)
   int last[2];  // this half's piece was the last of its group to arrive
 };
 static_assert(sizeof(PromptBars) <= 512, "barriers fit their place");
 
+// Waits at most two seconds, and not at all once another wait has run out.
+__device__ __forceinline__ uint64_t pr_clock_ns() {
+  uint64_t t;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+  return t;
+}
 __device__ __forceinline__ bool pr_wait(uint64_t* bar, uint32_t parity, PromptBars* s) {
   volatile int* dead = &s->dead;
-  for (uint32_t i = 0; i < (1u << 26); ++i) {
+  uint64_t start = 0;
+  for (uint32_t i = 1;; ++i) {
     if (mbar_try_wait(bar, parity)) return true;
-    if ((i & 255) == 255 && *dead) return false;
+    if ((i & 63) == 0) {
+      if (*dead) return false;
+      const uint64_t now = pr_clock_ns();
+      if (start == 0) start = now;
+      if (now - start > 2000000000ull) break;
+    }
   }
   *dead = 1;
   atomicOr(&g_prompt_status, SQ_DEV_TIMEOUT);
@@ -470,14 +491,19 @@ __global__ void __launch_bounds__(kPrThreads, 1)
   if (tid == 0) {
     mbar_init(&s->q_full, 1);
     mbar_init(&s->q_empty, 1);
-    for (int i = 0; i < kPrStages; ++i) {
-      mbar_init(&s->kv_full[i], 1);
-      mbar_init(&s->kv_empty[i], 1);
+    for (int i = 0; i < kPrK; ++i) {
+      mbar_init(&s->k_full[i], 1);
+      mbar_init(&s->k_empty[i], 1);
+    }
+    for (int i = 0; i < kPrV; ++i) {
+      mbar_init(&s->v_full[i], 1);
+      mbar_init(&s->v_empty[i], 1);
       mbar_init(&s->v_ready[i], 2);
     }
     for (int h = 0; h < 2; ++h) {
       mbar_init(&s->s_full[h], 1);
-      mbar_init(&s->p_ready[h], 128);
+      mbar_init(&s->p_ready[h][0], 4);
+      mbar_init(&s->p_ready[h][1], 4);
       mbar_init(&s->o_done[h], 1);
     }
     mbar_init(&s->drain, 1);
@@ -511,16 +537,16 @@ __global__ void __launch_bounds__(kPrThreads, 1)
    if (warp == 8) {
     if (lane == 0) {
       // ------------------------------------------------------------- TMA
-      uint32_t n = 0;  // tiles requested
+      // Every waiter of a barrier waits for each of its phases, so that a parity
+      // names one phase: keys and values have rings of their own.
+      uint32_t nk = 0, nv = 0;  // tiles requested
       bool fine = true;
-      auto tile = [&](const CUtensorMap* map, int blk, int bh) {
-        const uint32_t st = n % kPrStages;
-        if (!(fine = pr_wait(&s->kv_empty[st], ((n / kPrStages) & 1u) ^ 1u, s))) return;
-        const uint32_t dst = base + kPrOffKV + st * kPrTile;
-        mbar_arrive_expect_tx(&s->kv_full[st], kPrTile);
-        tma_load_3d(dst, map, 0, blk * kPrKeys, bh, &s->kv_full[st]);
-        tma_load_3d(dst + kPrTile / 2, map, 64, blk * kPrKeys, bh, &s->kv_full[st]);
-        ++n;
+      auto tile = [&](const CUtensorMap* map, uint64_t* full, uint64_t* empty, uint32_t dst, uint32_t lap, int blk,
+                      int bh) {
+        if (!(fine = pr_wait(empty, (lap & 1u) ^ 1u, s))) return;
+        mbar_arrive_expect_tx(full, kPrTile);
+        tma_load_3d(dst, map, 0, blk * kPrKeys, bh, full);
+        tma_load_3d(dst + kPrTile / 2, map, 64, blk * kPrKeys, bh, full);
       };
       int done = 0;  // items whose queries were requested
       for (int r = 0, w; fine && (w = pick(r)) < total; ++r) {
@@ -529,8 +555,10 @@ __global__ void __launch_bounds__(kPrThreads, 1)
         const int nb = max(pr_blocks(it, a.G, 0), pr_blocks(it, a.G, 1));
         const bool two = it.row0 + 128 < it.len * a.G;
         for (int j = 0; fine && j < nb; ++j) {
-          tile(&tk, it.blk0 + j, bh);
+          tile(&tk, &s->k_full[nk % kPrK], &s->k_empty[nk % kPrK], base + kPrOffKV + (nk % kPrK) * kPrTile, nk / kPrK,
+               it.blk0 + j, bh);
           if (!fine) break;
+          ++nk;
           if (j == 0) {
             if (!(fine = pr_wait(&s->q_empty, ((uint32_t)r & 1u) ^ 1u, s))) break;
             const int64_t y = ((int64_t)kvh * a.N + it.off) * a.G + it.row0;
@@ -540,14 +568,16 @@ __global__ void __launch_bounds__(kPrThreads, 1)
                 tma_load_2d(smem + h * kPrTile + c * (kPrTile / 2), &tq, 64 * c, (int)(y + 128 * h), &s->q_full);
             ++done;
           }
-          tile(&tv, it.blk0 + j, bh);
+          tile(&tv, &s->v_full[nv % kPrV], &s->v_empty[nv % kPrV], base + kPrOffKV + (kPrK + nv % kPrV) * kPrTile,
+               nv / kPrV, it.blk0 + j, bh);
+          if (fine) ++nv;
         }
       }
       if (!fine) {  // no copy may land after the CTA has left
-        for (uint32_t st = 0; st < kPrStages && st < n; ++st) {
-          const uint32_t last = st + (n - 1 - st) / kPrStages * kPrStages;
-          mbar_wait_bounded(&s->kv_full[st], (last / kPrStages) & 1u, 1u << 20);
-        }
+        for (uint32_t i = nk > kPrK ? nk - kPrK : 0; i < nk; ++i)
+          mbar_wait_bounded(&s->k_full[i % kPrK], (i / kPrK) & 1u, 1u << 20);
+        for (uint32_t i = nv > kPrV ? nv - kPrV : 0; i < nv; ++i)
+          mbar_wait_bounded(&s->v_full[i % kPrV], (i / kPrV) & 1u, 1u << 20);
         if (done) mbar_wait_bounded(&s->q_full, (uint32_t)(done - 1) & 1u, 1u << 20);
       }
     }
@@ -557,7 +587,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
       // D fp32, A and B fp16, M = N = 128; of the values N runs (bit 16)
       const uint32_t id_qk = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
       const uint32_t id_pv = id_qk | (1u << 16);
-      uint32_t n = 0;           // tiles taken
+      uint32_t nk = 0, nv = 0;  // tiles of keys, of values taken
       uint32_t np[2] = {0, 0};  // blocks of each half whose weights were waited for
       bool fine = true;
       auto qk = [&](int h, uint32_t st) {
@@ -573,40 +603,46 @@ __global__ void __launch_bounds__(kPrThreads, 1)
         const PromptItem it = items[w / a.Hkv];
         const int nb[2] = {pr_blocks(it, a.G, 0), pr_blocks(it, a.G, 1)};
         const int nm = max(nb[0], nb[1]);  // (never zero: the item's last row sees its last block)
-        auto stage = [&](uint32_t i) { return i % kPrStages; };
-        auto phase = [&](uint32_t i) { return (i / kPrStages) & 1u; };
-        // (v_ready has a phase per value tile: a stage holds one on every other pass, kPrStages is odd)
-        if (!(fine = pr_wait(&s->kv_full[stage(n)], phase(n), s) && pr_wait(&s->q_full, (uint32_t)r & 1u, s))) break;
+        auto keys = [&]() { return pr_wait(&s->k_full[nk % kPrK], (nk / kPrK) & 1u, s); };
+        if (!(fine = keys() && pr_wait(&s->q_full, (uint32_t)r & 1u, s))) break;
         tc_fence_after();
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-          if (nb[h] > 0) qk(h, stage(n));
-        tc_commit(&s->kv_empty[stage(n)]);
+          if (nb[h] > 0) qk(h, nk % kPrK);
+        tc_commit(&s->k_empty[nk % kPrK]);
+        ++nk;
         if (nm == 1) tc_commit(&s->q_empty);
         for (int j = 0; fine && j < nm; ++j) {
-          const uint32_t iv = n + 2 * j + 1, ik = iv + 1;
-          if (j + 1 < nm && !(fine = pr_wait(&s->kv_full[stage(ik)], phase(ik), s))) break;
-          if (!(fine = pr_wait(&s->v_ready[stage(iv)], (iv / (2 * kPrStages)) & 1u, s))) break;
-          const uint64_t vd = sw128_desc_mn(base + kPrOffKV + stage(iv) * kPrTile);
+          if (j + 1 < nm && !(fine = keys())) break;
+          if (!(fine = pr_wait(&s->v_ready[nv % kPrV], (nv / kPrV) & 1u, s))) break;
+          const uint64_t vd = sw128_desc_mn(base + kPrOffKV + (kPrK + nv % kPrV) * kPrTile);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             if (j >= nb[h]) continue;
-            if (!(fine = pr_wait(&s->p_ready[h], np[h] & 1u, s))) break;
-            ++np[h];
-            tc_fence_after();
+            // the first 64 keys' weights are there while the others are computed
 #pragma unroll
-            for (int kk = 0; kk < kPrKeys / 16; ++kk)
-              tc_mma_f16_ts(tmem + 256 + h * 128, tmem + h * 128 + kk * 8, vd + kk * (16 * 128 / 16), id_pv,
-                            j > 0 || kk > 0);
+            for (int half = 0; half < 2; ++half) {
+              if (!(fine = pr_wait(&s->p_ready[h][half], np[h] & 1u, s))) break;
+              tc_fence_after();
+#pragma unroll
+              for (int kk = 4 * half; kk < 4 * half + 4; ++kk)
+                tc_mma_f16_ts(tmem + 256 + h * 128, tmem + h * 128 + kk * 8, vd + kk * (16 * 128 / 16), id_pv,
+                              j > 0 || kk > 0);
+            }
+            if (!fine) break;
+            ++np[h];
             tc_commit(&s->o_done[h]);
-            if (j + 1 < nb[h]) qk(h, stage(ik));
+            if (j + 1 < nb[h]) qk(h, nk % kPrK);
           }
           if (!fine) break;
-          tc_commit(&s->kv_empty[stage(iv)]);
-          if (j + 1 < nm) tc_commit(&s->kv_empty[stage(ik)]);
+          tc_commit(&s->v_empty[nv % kPrV]);
+          ++nv;
+          if (j + 1 < nm) {
+            tc_commit(&s->k_empty[nk % kPrK]);
+            ++nk;
+          }
           if (j + 2 == nm) tc_commit(&s->q_empty);
         }
-        n += 2 * nm;
       }
       if (!fine) {  // what was issued still writes TMEM
         tc_commit(&s->drain);
@@ -620,40 +656,51 @@ __global__ void __launch_bounds__(kPrThreads, 1)
     // values of new tokens (their rows are marked), which go to the rows that
     // see them at the end, by themselves.
     const int t = tid - 320;
-    uint32_t n = 0;
+    uint32_t nv = 0;
     bool fine = true;
     for (int r = 0, w; fine && (w = pick(r)) < total; ++r) {
       const PromptItem it = items[w / a.Hkv];
       const uint8_t* odd = a.work->odd + (int64_t)(w % a.Hkv) * a.N + it.off;
       const int nb = max(pr_blocks(it, a.G, 0), pr_blocks(it, a.G, 1)), end = it.pos0 + it.len;
-      for (int j = 0; j < nb; ++j, n += 2) {
-        const uint32_t st = (n + 1) % kPrStages, ph = ((n + 1) / kPrStages) & 1u;
-        const int key0 = (it.blk0 + j) * kPrKeys;
-        bool marked[2];
+      // the marks of a block are read a block ahead: what a tile waits for here is
+      // in the chain of every tile (with the read in it, and a fence that nothing
+      // needed: 8000 tokens 40 / 8 heads 656 us)
+      auto marks = [&](int j) {
+        uint32_t m = 0;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const int key = key0 + t + 64 * e;
-          marked[e] = key >= it.pos0 && key < end && odd[key - it.pos0];
+          const int key = (it.blk0 + j) * kPrKeys + t + 64 * e;
+          if (j < nb && key >= it.pos0 && key < end && odd[key - it.pos0]) m |= 1u << e;
         }
-        fine = __all_sync(0xffffffffu, pr_wait(&s->kv_full[st], ph, s));
+        return m;
+      };
+      uint32_t next = marks(0);
+      for (int j = 0; j < nb; ++j, ++nv) {
+        const uint32_t st = nv % kPrV, ph = (nv / kPrV) & 1u;
+        const int key0 = (it.blk0 + j) * kPrKeys;
+        const uint32_t marked = next;
+        next = marks(j + 1);
+        fine = __all_sync(0xffffffffu, pr_wait(&s->v_full[st], ph, s));
         if (!fine) break;
-        uint8_t* v = smem + kPrOffKV + st * kPrTile;
         const int gone = min(max(key0 + kPrKeys - end, 0), kPrKeys);
-        for (int i = t; i < gone * 16; i += 64)
-          *reinterpret_cast<uint4*>(v + ((i >> 3) & 1) * (kPrTile / 2) + (kPrKeys - gone + (i >> 4)) * 128 +
-                                    (i & 7) * 16) = make_uint4(0, 0, 0, 0);
+        if (__any_sync(0xffffffffu, gone > 0 || marked)) {
+          uint8_t* v = smem + kPrOffKV + (kPrK + st) * kPrTile;
+          for (int i = t; i < gone * 16; i += 64)
+            *reinterpret_cast<uint4*>(v + ((i >> 3) & 1) * (kPrTile / 2) + (kPrKeys - gone + (i >> 4)) * 128 +
+                                      (i & 7) * 16) = make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-          if (marked[e]) {
-            for (int c = 0; c < 2; ++c)
-              for (int d = 0; d < 64; ++d) {
-                uint16_t* x = reinterpret_cast<uint16_t*>(v + c * (kPrTile / 2) + (t + 64 * e) * 128) + d;
-                if ((*x & 0x7c00u) == 0x7c00u) *x = 0;
-              }
-            *(volatile int*)&s->odd[r & 7] = r + 1;
-          }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
+          for (int e = 0; e < 2; ++e)
+            if ((marked >> e) & 1) {
+              for (int c = 0; c < 2; ++c)
+                for (int d = 0; d < 64; ++d) {
+                  uint16_t* x = reinterpret_cast<uint16_t*>(v + c * (kPrTile / 2) + (t + 64 * e) * 128) + d;
+                  if ((*x & 0x7c00u) == 0x7c00u) *x = 0;
+                }
+              *(volatile int*)&s->odd[r & 7] = r + 1;
+            }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+        }
         if (lane == 0) mbar_arrive(&s->v_ready[st]);
       }
     }
@@ -682,25 +729,39 @@ __global__ void __launch_bounds__(kPrThreads, 1)
         if (j > 0) pr_wait(&s->o_done[h], (ns & 1u) ^ 1u, s);
         __syncwarp();
         tc_fence_after();
+        // scores in two loads, the second under the first one's maximum
         uint32_t v[128];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tm_ld32(ts + 32 * i, v + 32 * i);
-        tm_wait_ld();
         const int key0 = (it.blk0 + j) * kPrKeys;
-        if (key0 + kPrKeys - 1 > first) {
-          const int seen = pos - key0;  // the last key this row sees
-#pragma unroll
-          for (int i = 0; i < 128; ++i)
-            if (i > seen) v[i] = 0xff800000u;
-        }
+        const bool edge = key0 + kPrKeys - 1 > first;
+        const int seen = pos - key0;  // the last key this row sees
         float mx[4];
+        tm_ld32(ts, v);
+        tm_ld32(ts + 32, v + 32);
+        tm_wait_ld();
+        tm_loaded32(v);
+        tm_loaded32(v + 32);
+        tm_ld32(ts + 64, v + 64);
+        tm_ld32(ts + 96, v + 96);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) mx[i] = fmaxf(__uint_as_float(v[i]), __uint_as_float(v[i + 4]));
+        for (int i = 0; i < 2; ++i) {
+          if (i) {
+            tm_wait_ld();
+            tm_loaded32(v + 64);
+            tm_loaded32(v + 96);
+          }
+          if (edge) {
 #pragma unroll
-        for (int i = 8; i < 128; i += 8)
+            for (int e = 64 * i; e < 64 * i + 64; ++e)
+              if (e > seen) v[e] = 0xff800000u;
+          }
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            mx[e] = fmaxf(fmaxf(mx[e], __uint_as_float(v[i + e])), __uint_as_float(v[i + 4 + e]));
+          for (int e = 64 * i; e < 64 * i + 64; e += 8)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float x = __uint_as_float(v[e + k]), y = __uint_as_float(v[e + 4 + k]);
+              mx[k] = e == 0 ? fmaxf(x, y) : fmaxf(fmaxf(mx[k], x), y);
+            }
+        }
         const float mb = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
         if (__any_sync(0xffffffffu, (mb - m) * c > kPrSlack)) {
           const float mn = fmaxf(m, mb);
@@ -714,6 +775,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
               uint32_t o[32];
               tm_ld32(to + 32 * i, o);
               tm_wait_ld();
+              tm_loaded32(o);
 #pragma unroll
               for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
               tm_st32(to + 32 * i, o);
@@ -735,11 +797,12 @@ __global__ void __launch_bounds__(kPrThreads, 1)
             p[e] = pack_f16x2(p0, p1);
           }
           tm_st32(ts + 32 * i, p);
+          tm_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&s->p_ready[h][i]);  // (32 arrivals of a warp take turns)
         }
         l2 = fadd2(sum[0], sum[1]);
-        tm_wait_st();
-        tc_fence_before();
-        mbar_arrive(&s->p_ready[h]);
       }
       // ---- the rows' results
       if (nb > 0) pr_wait(&s->o_done[h], (ns & 1u) ^ 1u, s);
@@ -758,6 +821,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
         if (nb > 0) {
           tm_ld32(to + 32 * i, o);
           tm_wait_ld();
+          tm_loaded32(o);
         }
 #pragma unroll
         for (int e = 0; e < 32; ++e) o[e] = nb > 0 ? __float_as_uint(__uint_as_float(o[e]) * f) : 0u;
