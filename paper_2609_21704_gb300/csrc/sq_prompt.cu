@@ -15,6 +15,7 @@
 #include "sq_tcgen.cuh"
 
 #include <mutex>
+#include <stddef.h>
 
 namespace sq {
 
@@ -87,14 +88,22 @@ struct PlanArgs {
   PromptWork init;
 };
 
+// The batch's offsets and positions, in shared memory where they fit (the plan
+// walks them five times, and every walk would wait for memory).
+constexpr int kPlanSeqs = 512;
+struct PlanBatch {
+  int off[kPlanSeqs + 1], pos[kPlanSeqs];
+};
+
 // Calls f(b, off, len, p0, row0, blocks) for every tile of every sequence that
 // fits its cache; a warp a sequence, a lane a tile.
 template <typename F>
-__device__ __forceinline__ void for_tiles(const PlanArgs& a, F f) {
+__device__ __forceinline__ void for_tiles(const PlanArgs& a, const PlanBatch& s, F f) {
   const int lane = threadIdx.x & 31;
+  const bool near = a.pk.B <= kPlanSeqs;
   for (int b = threadIdx.x >> 5; b < a.pk.B; b += blockDim.x >> 5) {
-    const int off = a.pk.offsets[b], len = a.pk.offsets[b + 1] - off;
-    const int64_t p0 = a.pk.pos0[b];
+    const int off = near ? s.off[b] : a.pk.offsets[b], len = (near ? s.off[b + 1] : a.pk.offsets[b + 1]) - off;
+    const int64_t p0 = near ? s.pos[b] : a.pk.pos0[b];
     if (p0 < 0 || p0 + len > a.pk.max_ctx) continue;
     const int64_t rows = (int64_t)len * a.G;
     for (int64_t r = (int64_t)lane * kPrRows; r < rows; r += 32 * kPrRows) {
@@ -107,23 +116,31 @@ __device__ __forceinline__ void for_tiles(const PlanArgs& a, F f) {
 
 // Tiles in order of falling cost, so that the persistent CTAs, who take items in
 // turn, end together.  Few tiles (a short chunk behind a long prefix) are cut
-// along the keys: of one to three rounds over the SMs, or none, the cheapest by
-// rounds x (blocks a piece + 2 for what a piece costs besides).
+// along the keys: of pieces of half to twice an SM's even share of the blocks, or
+// no cut, the cheapest by rounds over the SMs x (blocks of the longest piece + 3
+// for what a piece costs besides).
+constexpr int kPlanCuts = 13;
 __device__ void prompt_plan(const PlanArgs& a) {
   __shared__ unsigned int start[kPrMaxBlocks + 1];
   __shared__ unsigned long long total;
-  __shared__ unsigned int tiles, longest, pieces[4], items, groups, recs, warp_sum_[8];
+  __shared__ unsigned int tiles, longest, pieces[kPlanCuts], piece[kPlanCuts], items, groups, recs, warp_sum_[8];
+  __shared__ PlanBatch batch;
   const int tid = threadIdx.x;
   bool bad = false;
   for (int b = tid; b < a.pk.B; b += blockDim.x) {
     const int lo = a.pk.offsets[b], hi = a.pk.offsets[b + 1];
     bad |= lo < 0 || hi < lo || (int64_t)hi > a.pk.N;
+    if (b < kPlanSeqs) {
+      batch.off[b] = lo;
+      batch.off[b + 1] = hi;  // (the next sequence's thread writes the same)
+      batch.pos[b] = a.pk.pos0[b];
+    }
   }
   if (tid == 0) {
     total = 0;
     tiles = longest = items = groups = recs = 0;
-    pieces[0] = pieces[1] = pieces[2] = pieces[3] = 0;
   }
+  if (tid < kPlanCuts) pieces[tid] = piece[tid] = 0;
   for (int i = tid; i <= kPrMaxBlocks; i += blockDim.x) start[i] = 0;
   if (__syncthreads_or(bad)) {
     if (tid == 0) {
@@ -132,7 +149,7 @@ __device__ void prompt_plan(const PlanArgs& a) {
     }
     return;
   }
-  for_tiles(a, [&](int, int, int, int, int, int blocks) {
+  for_tiles(a, batch, [&](int, int, int, int, int, int blocks) {
     atomicAdd(&total, (unsigned long long)blocks);
     atomicAdd(&tiles, 1u);
     atomicMax(&longest, (unsigned)blocks);
@@ -140,30 +157,31 @@ __device__ void prompt_plan(const PlanArgs& a) {
   __syncthreads();
   unsigned int chunk = kPrMaxBlocks + 1;
   if ((int64_t)tiles * a.Hkv < a.max_pieces && longest > 2) {
-    unsigned int c[4];
-    for (int w = 1; w <= 3; ++w) {
-      const unsigned long long per = (total * a.Hkv + (unsigned)(a.sms * w) - 1) / (unsigned)(a.sms * w);
-      c[w] = per < 2 ? 2u : (unsigned)per;
-    }
-    for_tiles(a, [&](int, int, int, int, int, int blocks) {
-      for (int w = 1; w <= 3; ++w) atomicAdd(&pieces[w], ((unsigned)blocks + c[w] - 1) / c[w]);
+    const unsigned int even = (unsigned int)((total * a.Hkv + (unsigned)a.sms - 1) / (unsigned)a.sms);
+    auto cut = [&](int i) { return max(2u, (even * (4 + i) + 7) / 8); };
+    for_tiles(a, batch, [&](int, int, int, int, int, int blocks) {
+      for (int i = 0; i < kPlanCuts; ++i) {
+        const unsigned int S = ((unsigned)blocks + cut(i) - 1) / cut(i);
+        atomicAdd(&pieces[i], S);
+        atomicMax(&piece[i], ((unsigned)blocks + S - 1) / S);
+      }
     });
     __syncthreads();
-    // unsplit: the longest tile, or the tiles in rounds of their mean
+    // uncut: the longest tile, or the tiles in rounds of their mean
     unsigned long long best = (unsigned long long)longest + 2;
     const unsigned long long rounds = ((unsigned long long)tiles * a.Hkv + a.sms - 1) / a.sms;
     if (rounds > 1) best = max(best, rounds * (total / tiles + 2));
-    for (int w = 1; w <= 3; ++w) {
-      const unsigned long long n = (unsigned long long)pieces[w] * a.Hkv;
-      const unsigned long long cost = (n + a.sms - 1) / a.sms * (min(c[w], longest) + 3);
+    for (int i = 0; i < kPlanCuts; ++i) {
+      const unsigned long long n = (unsigned long long)pieces[i] * a.Hkv;
+      const unsigned long long cost = (n + a.sms - 1) / a.sms * (piece[i] + 3);
       if ((int64_t)n <= a.max_pieces && cost < best) {
         best = cost;
-        chunk = c[w];
+        chunk = cut(i);
       }
     }
   }
   // counting sort by the blocks of a piece
-  for_tiles(a, [&](int, int, int, int, int, int blocks) {
+  for_tiles(a, batch, [&](int, int, int, int, int, int blocks) {
     const unsigned int S = ((unsigned)blocks + chunk - 1) / chunk;
     atomicAdd(&start[((unsigned)blocks + S - 1) / S], S);
   });
@@ -196,7 +214,7 @@ __device__ void prompt_plan(const PlanArgs& a) {
     }
   }
   __syncthreads();
-  for_tiles(a, [&](int b, int off, int len, int p0, int row0, int blocks) {
+  for_tiles(a, batch, [&](int b, int off, int len, int p0, int row0, int blocks) {
     const unsigned int S = ((unsigned)blocks + chunk - 1) / chunk;
     const unsigned int at = atomicAdd(&start[((unsigned)blocks + S - 1) / S], S);
     PromptItem it = {b, off, len, p0, row0, 0, 0, 0, (int)S, -1, -1, 0};
@@ -320,11 +338,18 @@ __global__ void __launch_bounds__(kPrPrepThreads) prompt_prepare_kernel(
 // ---- attention -----------------------------------------------------------------
 
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2,
-                                            uint64_t* bar) {
+                                            uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
       " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(smem_u32(bar))
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_q(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(bar)
       : "memory");
 }
 
@@ -443,11 +468,25 @@ __device__ __forceinline__ uint64_t pr_clock_ns() {
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
   return t;
 }
-__device__ __forceinline__ bool pr_wait(uint64_t* bar, uint32_t parity, PromptBars* s) {
+// (barriers by their shared address: the roles' registers are few)
+__device__ __forceinline__ bool pr_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+      "selp.u32 %0, 1, 0, p;\n"
+      "}\n"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ bool pr_wait(uint32_t bar, uint32_t parity, PromptBars* s) {
   volatile int* dead = &s->dead;
   uint64_t start = 0;
   for (uint32_t i = 1;; ++i) {
-    if (mbar_try_wait(bar, parity)) return true;
+    if (pr_try(bar, parity)) return true;
     if ((i & 63) == 0) {
       if (*dead) return false;
       const uint64_t now = pr_clock_ns();
@@ -458,6 +497,15 @@ __device__ __forceinline__ bool pr_wait(uint64_t* bar, uint32_t parity, PromptBa
   *dead = 1;
   atomicOr(&g_prompt_status, SQ_DEV_TIMEOUT);
   return false;
+}
+__device__ __forceinline__ void pr_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void pr_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void pr_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
 // The blocks of an item that half h of its rows sees any key of.
@@ -487,6 +535,8 @@ __global__ void __launch_bounds__(kPrThreads, 1)
   uint8_t* smem = pr_raw + (((smem_u32(pr_raw) + 1023u) & ~1023u) - smem_u32(pr_raw));
   PromptBars* s = reinterpret_cast<PromptBars*>(smem + kPrOffBar);
   const uint32_t base = smem_u32(smem);
+#define PR_BAR(member) (bars + (uint32_t)offsetof(PromptBars, member))
+  const uint32_t bars = base + kPrOffBar;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     mbar_init(&s->q_full, 1);
@@ -533,7 +583,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
   // registers: 384 threads x 168 at launch; the softmax groups take 216, the
   // others keep 72 (256 x 216 + 128 x 72 = 384 x 168)
   if (warp >= 8) {
-   asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+   asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
    if (warp == 8) {
     if (lane == 0) {
       // ------------------------------------------------------------- TMA
@@ -541,10 +591,10 @@ __global__ void __launch_bounds__(kPrThreads, 1)
       // names one phase: keys and values have rings of their own.
       uint32_t nk = 0, nv = 0;  // tiles requested
       bool fine = true;
-      auto tile = [&](const CUtensorMap* map, uint64_t* full, uint64_t* empty, uint32_t dst, uint32_t lap, int blk,
+      auto tile = [&](const CUtensorMap* map, uint32_t full, uint32_t empty, uint32_t dst, uint32_t lap, int blk,
                       int bh) {
         if (!(fine = pr_wait(empty, (lap & 1u) ^ 1u, s))) return;
-        mbar_arrive_expect_tx(full, kPrTile);
+        pr_expect(full, kPrTile);
         tma_load_3d(dst, map, 0, blk * kPrKeys, bh, full);
         tma_load_3d(dst + kPrTile / 2, map, 64, blk * kPrKeys, bh, full);
       };
@@ -555,20 +605,20 @@ __global__ void __launch_bounds__(kPrThreads, 1)
         const int nb = max(pr_blocks(it, a.G, 0), pr_blocks(it, a.G, 1));
         const bool two = it.row0 + 128 < it.len * a.G;
         for (int j = 0; fine && j < nb; ++j) {
-          tile(&tk, &s->k_full[nk % kPrK], &s->k_empty[nk % kPrK], base + kPrOffKV + (nk % kPrK) * kPrTile, nk / kPrK,
+          tile(&tk, PR_BAR(k_full) + 8 * (nk % kPrK), PR_BAR(k_empty) + 8 * (nk % kPrK), base + kPrOffKV + (nk % kPrK) * kPrTile, nk / kPrK,
                it.blk0 + j, bh);
           if (!fine) break;
           ++nk;
           if (j == 0) {
-            if (!(fine = pr_wait(&s->q_empty, ((uint32_t)r & 1u) ^ 1u, s))) break;
+            if (!(fine = pr_wait(PR_BAR(q_empty), ((uint32_t)r & 1u) ^ 1u, s))) break;
             const int64_t y = ((int64_t)kvh * a.N + it.off) * a.G + it.row0;
-            mbar_arrive_expect_tx(&s->q_full, two ? 2 * kPrTile : kPrTile);
+            pr_expect(PR_BAR(q_full), two ? 2 * kPrTile : kPrTile);
             for (int h = 0; h < (two ? 2 : 1); ++h)
               for (int c = 0; c < 2; ++c)
-                tma_load_2d(smem + h * kPrTile + c * (kPrTile / 2), &tq, 64 * c, (int)(y + 128 * h), &s->q_full);
+                tma_load_q(base + h * kPrTile + c * (kPrTile / 2), &tq, 64 * c, (int)(y + 128 * h), PR_BAR(q_full));
             ++done;
           }
-          tile(&tv, &s->v_full[nv % kPrV], &s->v_empty[nv % kPrV], base + kPrOffKV + (kPrK + nv % kPrV) * kPrTile,
+          tile(&tv, PR_BAR(v_full) + 8 * (nv % kPrV), PR_BAR(v_empty) + 8 * (nv % kPrV), base + kPrOffKV + (kPrK + nv % kPrV) * kPrTile,
                nv / kPrV, it.blk0 + j, bh);
           if (fine) ++nv;
         }
@@ -597,24 +647,24 @@ __global__ void __launch_bounds__(kPrThreads, 1)
           const uint64_t o = (uint64_t)((kk >> 2) * (kPrTile / 2 / 16) + (kk & 3) * 2);
           tc_mma_f16(tmem + h * 128, qd + o, kd + o, id_qk, kk > 0);
         }
-        tc_commit(&s->s_full[h]);
+        pr_commit(PR_BAR(s_full) + 8 * (h));
       };
       for (int r = 0, w; fine && (w = pick(r)) < total; ++r) {
         const PromptItem it = items[w / a.Hkv];
         const int nb[2] = {pr_blocks(it, a.G, 0), pr_blocks(it, a.G, 1)};
         const int nm = max(nb[0], nb[1]);  // (never zero: the item's last row sees its last block)
-        auto keys = [&]() { return pr_wait(&s->k_full[nk % kPrK], (nk / kPrK) & 1u, s); };
-        if (!(fine = keys() && pr_wait(&s->q_full, (uint32_t)r & 1u, s))) break;
+        auto keys = [&]() { return pr_wait(PR_BAR(k_full) + 8 * (nk % kPrK), (nk / kPrK) & 1u, s); };
+        if (!(fine = keys() && pr_wait(PR_BAR(q_full), (uint32_t)r & 1u, s))) break;
         tc_fence_after();
 #pragma unroll
         for (int h = 0; h < 2; ++h)
           if (nb[h] > 0) qk(h, nk % kPrK);
-        tc_commit(&s->k_empty[nk % kPrK]);
+        pr_commit(PR_BAR(k_empty) + 8 * (nk % kPrK));
         ++nk;
-        if (nm == 1) tc_commit(&s->q_empty);
+        if (nm == 1) pr_commit(PR_BAR(q_empty));
         for (int j = 0; fine && j < nm; ++j) {
           if (j + 1 < nm && !(fine = keys())) break;
-          if (!(fine = pr_wait(&s->v_ready[nv % kPrV], (nv / kPrV) & 1u, s))) break;
+          if (!(fine = pr_wait(PR_BAR(v_ready) + 8 * (nv % kPrV), (nv / kPrV) & 1u, s))) break;
           const uint64_t vd = sw128_desc_mn(base + kPrOffKV + (kPrK + nv % kPrV) * kPrTile);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
@@ -622,7 +672,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
             // the first 64 keys' weights are there while the others are computed
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-              if (!(fine = pr_wait(&s->p_ready[h][half], np[h] & 1u, s))) break;
+              if (!(fine = pr_wait(PR_BAR(p_ready) + 16 * (h) + 8 * (half), np[h] & 1u, s))) break;
               tc_fence_after();
 #pragma unroll
               for (int kk = 4 * half; kk < 4 * half + 4; ++kk)
@@ -631,21 +681,21 @@ __global__ void __launch_bounds__(kPrThreads, 1)
             }
             if (!fine) break;
             ++np[h];
-            tc_commit(&s->o_done[h]);
+            pr_commit(PR_BAR(o_done) + 8 * (h));
             if (j + 1 < nb[h]) qk(h, nk % kPrK);
           }
           if (!fine) break;
-          tc_commit(&s->v_empty[nv % kPrV]);
+          pr_commit(PR_BAR(v_empty) + 8 * (nv % kPrV));
           ++nv;
           if (j + 1 < nm) {
-            tc_commit(&s->k_empty[nk % kPrK]);
+            pr_commit(PR_BAR(k_empty) + 8 * (nk % kPrK));
             ++nk;
           }
-          if (j + 2 == nm) tc_commit(&s->q_empty);
+          if (j + 2 == nm) pr_commit(PR_BAR(q_empty));
         }
       }
       if (!fine) {  // what was issued still writes TMEM
-        tc_commit(&s->drain);
+        pr_commit(PR_BAR(drain));
         mbar_wait_bounded(&s->drain, 0u, 1u << 20);
       }
     }
@@ -680,7 +730,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
         const int key0 = (it.blk0 + j) * kPrKeys;
         const uint32_t marked = next;
         next = marks(j + 1);
-        fine = __all_sync(0xffffffffu, pr_wait(&s->v_full[st], ph, s));
+        fine = __all_sync(0xffffffffu, pr_wait(PR_BAR(v_full) + 8 * (st), ph, s));
         if (!fine) break;
         const int gone = min(max(key0 + kPrKeys - end, 0), kPrKeys);
         if (__any_sync(0xffffffffu, gone > 0 || marked)) {
@@ -701,12 +751,12 @@ __global__ void __launch_bounds__(kPrThreads, 1)
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
         }
-        if (lane == 0) mbar_arrive(&s->v_ready[st]);
+        if (lane == 0) pr_arrive(PR_BAR(v_ready) + 8 * (st));
       }
     }
    }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     // ------------------------------------------------------------- softmax
     const int h = warp >> 2, row = tid & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
@@ -725,8 +775,8 @@ __global__ void __launch_bounds__(kPrThreads, 1)
       float m = -INFINITY;
       unsigned long long l2 = 0;  // the sum, two halves
       for (int j = 0; j < nb; ++j, ++ns) {
-        pr_wait(&s->s_full[h], ns & 1u, s);
-        if (j > 0) pr_wait(&s->o_done[h], (ns & 1u) ^ 1u, s);
+        pr_wait(PR_BAR(s_full) + 8 * (h), ns & 1u, s);
+        if (j > 0) pr_wait(PR_BAR(o_done) + 8 * (h), (ns & 1u) ^ 1u, s);
         __syncwarp();
         tc_fence_after();
         // scores in two loads, the second under the first one's maximum
@@ -800,12 +850,12 @@ __global__ void __launch_bounds__(kPrThreads, 1)
           tm_wait_st();
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(&s->p_ready[h][i]);  // (32 arrivals of a warp take turns)
+          if (lane == 0) pr_arrive(PR_BAR(p_ready) + 16 * (h) + 8 * (i));  // (32 arrivals of a warp take turns)
         }
         l2 = fadd2(sum[0], sum[1]);
       }
       // ---- the rows' results
-      if (nb > 0) pr_wait(&s->o_done[h], (ns & 1u) ^ 1u, s);
+      if (nb > 0) pr_wait(PR_BAR(o_done) + 8 * (h), (ns & 1u) ^ 1u, s);
       __syncwarp();
       tc_fence_after();
       const float2 lp = f2unpack(l2);
