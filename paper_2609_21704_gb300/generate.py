@@ -28,17 +28,14 @@ import numpy as np
 import torch
 
 from . import (SQ_ACCEPT_GREEDY, SQ_ACCEPT_SAMPLE, sq_accept_logits, sq_accept_logits_workspace_bytes,
-               sq_check, sq_embed, sq_sample_logits, sq_spec_commit, sq_spec_drafts, synth)
-from .stack import DecoderState, LinearStack, decoder_pass
+               sq_check, sq_embed, sq_logprobs, sq_sample_logits, sq_spec_commit, sq_spec_drafts, synth)
+from .stack import (HEAD_DIM, LINEAR_MAX_ROWS, DecoderState, LinearStack, PromptState, decoder_pass,
+                    prompt_pass)
 
 # Limits of one sq_attention call (see its declaration): at most 32 new
 # tokens per sequence, and (Hq / Hkv) * T <= 200 queries per key/value head.
 ATTN_MAX_T = 32
 ATTN_MAX_GROUP_QUERIES = 200
-
-
-# Rows of one linear call (sq_linear_ex): B sequences x T tokens of a pass.
-LINEAR_MAX_ROWS = 256
 
 
 def prefill_chunk(q_heads: int, kv_heads: int, B: int = 1) -> int:
@@ -51,11 +48,14 @@ class Generator:
     """Generation for B sequences over `stack` (which must hold the draft
     variant and an lm_head).  K >= 1: speculative cycles with `draft`
     drafting and `verifier` verifying; K = 0: direct decoding with
-    `verifier`, one token per cycle."""
+    `verifier`, one token per cycle.  draft_kv / verifier_kv "int4" keep that
+    model's cache in 4 bits.  Prompts: prefill (all of prompt_len tokens, in
+    passes of at most 32 of each) or prefill_packed (any lengths up to it, in
+    one pass)."""
 
     def __init__(self, stack: LinearStack, B: int, K: int, prompt_len: int, max_ctx: int,
                  draft: str = "int4", verifier: str = "fp16", mode: int = SQ_ACCEPT_GREEDY,
-                 temperature: float = 1.0, seed: int = 0):
+                 temperature: float = 1.0, seed: int = 0, draft_kv: str = "fp16", verifier_kv: str = "fp16"):
         if stack.lm_head is None:
             raise ValueError("generation needs the lm_head")
         if K < 0 or K > 16 or prompt_len < 1:
@@ -71,10 +71,10 @@ class Generator:
         i32 = dict(dtype=torch.int32, device=dev)
 
         # one cache per model; states per T share it
-        self.tv = DecoderState(stack, B, K + 1, max_ctx, seed=seed + 5)
+        self.tv = DecoderState(stack, B, K + 1, max_ctx, seed=seed + 5, kv=verifier_kv)
         self.d2 = self.d1 = None
         if K > 0:
-            self.d2 = DecoderState(stack, B, 2, max_ctx, share_gains=self.tv)
+            self.d2 = DecoderState(stack, B, 2, max_ctx, share_gains=self.tv, kv=draft_kv)
             if K > 1:
                 self.d1 = DecoderState(stack, B, 1, max_ctx, share=self.d2)
         pc = prefill_chunk(sh.q_heads, sh.kv_heads, B)
@@ -110,6 +110,7 @@ class Generator:
         self.ws_acc = torch.zeros(sq_accept_logits_workspace_bytes(B, K, V), dtype=torch.uint8, device=dev)
         self._graph = None
         self._cycles = 0
+        self._packed = None     # buffers of prefill_packed
 
     # ---- steps ------------------------------------------------------------------
     def _pick(self, z, u, out, stream):
@@ -151,6 +152,47 @@ class Generator:
                     sq_embed(chunk, self.table, sd.x, stream)
                     decoder_pass(self.stack, self.draft, sd, stream, pos0=self.chunk_pos[s],
                                  with_logits=False)
+            self.u1.copy_(torch.from_numpy(synth.uniforms(self.seed ^ 0x9F1, (B, 1))).to(dev))
+            self._pick(self.z1, self.u1, self.tok1, stream)
+            sq_spec_commit(None, self.tok1, self.hist, self.len, self.pos, self.last2, self.K, stream)
+
+    def prefill_packed(self, prompts, stream: torch.cuda.Stream) -> None:
+        """As prefill, from B prompts of different lengths (sequences of token
+        ids, 1 to prompt_len of each) in one pass of each model over all of
+        their tokens, packed one behind the other."""
+        B, dev = self.B, self.stack.device
+        lens = [len(p) for p in prompts]
+        if len(lens) != B or min(lens) < 1 or max(lens) > self.P:
+            raise ValueError(f"need {B} prompts of 1 to {self.P} tokens, got lengths {lens}")
+        rows = B * self.P
+        with torch.cuda.stream(stream):
+            if self._packed is None:
+                st = PromptState(self.stack, rows, B, self.max_ctx, logit_rows=B)
+                scratch = None
+                if self.tv.kv == "int4" or (self.d2 is not None and self.d2.kv == "int4"):
+                    shape = (B, self.stack.shape.kv_heads, self.max_ctx, HEAD_DIM)
+                    scratch = tuple(torch.zeros(shape, dtype=torch.float16, device=dev) for _ in range(2))
+                self._packed = (st, scratch)
+            st, scratch = self._packed
+            ids = np.zeros(rows, np.int32)
+            hist = np.zeros((B, self.P), np.int32)
+            off = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+            for b, p in enumerate(prompts):
+                ids[off[b]:off[b + 1]] = hist[b, :lens[b]] = np.asarray(p, np.int32)
+            ids_t = torch.from_numpy(ids).to(dev)
+            st.offsets.copy_(torch.from_numpy(off))
+            st.pos0.zero_()
+            last = torch.from_numpy(off[1:] - 1).to(dev)
+            self.hist.zero_()
+            self.hist[:, :self.P] = torch.from_numpy(hist).to(dev)
+            self.len.copy_(torch.tensor(lens, dtype=torch.int32))
+            self._cycles = 0
+            sq_embed(ids_t, self.table, st.x, stream)
+            prompt_pass(self.stack, self.verifier, st, self.tv, stream, scratch, logit_rows=last)
+            self.z1.copy_(st.logits)
+            if self.K > 0:
+                sq_embed(ids_t, self.table, st.x, stream)
+                prompt_pass(self.stack, self.draft, st, self.d2, stream, scratch)
             self.u1.copy_(torch.from_numpy(synth.uniforms(self.seed ^ 0x9F1, (B, 1))).to(dev))
             self._pick(self.z1, self.u1, self.tok1, stream)
             sq_spec_commit(None, self.tok1, self.hist, self.len, self.pos, self.last2, self.K, stream)
@@ -229,3 +271,40 @@ class Generator:
 
     def status(self) -> int:
         return sq_check()
+
+
+def score_prompts(stack: LinearStack, prompts, variant: str = "fp16", top: int = 0, temperature: float = 1.0,
+                  seed: int = 0, stream: torch.cuda.Stream | None = None):
+    """What the model makes of given texts, in one pass over all of them packed:
+    per prompt of n tokens the log probabilities fp32 [n - 1] of its tokens 2 ..
+    n given those before, the entropies [n - 1] of those predictions, and, with
+    top > 0, their `top` likeliest tokens int32 [n - 1, top] and log
+    probabilities.  A list of (logprob, entropy, top_tokens, top_logprobs) on
+    the device."""
+    if stack.lm_head is None:
+        raise ValueError("scoring needs the lm_head")
+    lens = [len(p) for p in prompts]
+    if not lens or min(lens) < 1:
+        raise ValueError("prompts of at least one token")
+    dev = stack.device
+    B, rows = len(lens), sum(lens)
+    off = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    ids = np.concatenate([np.asarray(p, np.int32) for p in prompts])
+    asked = np.concatenate([np.arange(a, b - 1, dtype=np.int32) for a, b in zip(off[:-1], off[1:])])
+    n = len(asked)
+    stream = torch.cuda.current_stream() if stream is None else stream
+    with torch.cuda.stream(stream):
+        cache = DecoderState(stack, B, 1, max(lens), seed=seed + 5)
+        st = PromptState(stack, rows, B, max(lens), logit_rows=n)
+        st.offsets.copy_(torch.from_numpy(off))
+        sq_embed(torch.from_numpy(ids).to(dev), stack.embedding(), st.x, stream)
+        f32 = dict(dtype=torch.float32, device=dev)
+        lp, ent, tl = torch.empty(n, **f32), torch.empty(n, **f32), torch.empty((n, top), **f32)
+        tt = torch.empty((n, top), dtype=torch.int32, device=dev)
+        if n:
+            rows_t = torch.from_numpy(asked).to(dev)
+            prompt_pass(stack, variant, st, cache, stream, logit_rows=rows_t)
+            sq_logprobs(st.logits, temperature, torch.from_numpy(ids[asked + 1]).to(dev), lp, ent,
+                        tt if top else None, tl if top else None, stream)
+    at = np.concatenate([[0], np.cumsum([k - 1 for k in lens])])
+    return [(lp[a:b], ent[a:b], tt[a:b], tl[a:b]) for a, b in zip(at[:-1], at[1:])]

@@ -205,18 +205,26 @@ class DecoderState:
     RMSNorm gains, the residual stream and the pass's activations.  Token t
     of sequence b sits at position pos0[b] + t.  `share` gives another
     state whose caches and gains this one uses (states of one model at
-    different T); `share_gains` gives only the gains (a second model)."""
+    different T); `share_gains` gives only the gains (a second model).
+    kv "int4" keeps the caches in 4 bits (sq_kv4_append): per layer (k_codes,
+    k_params, v_codes, v_params) in `kv4`, a quarter of the bytes."""
 
     def __init__(self, stack: LinearStack, B: int, T: int, max_ctx: int, context: int = 0,
                  seed: int = 5, share: "DecoderState | None" = None,
-                 share_gains: "DecoderState | None" = None):
-        from . import sq_attention_workspace_bytes
+                 share_gains: "DecoderState | None" = None, kv: str = "fp16"):
+        from . import sq_attention_kv4_workspace_bytes, sq_attention_workspace_bytes
         sh, dev = stack.shape, stack.device
         self.B, self.T, self.max_ctx = B, T, max_ctx
         nl = len(stack.layers)
+        if kv not in ("fp16", "int4"):
+            raise ValueError(f"kv must be 'fp16' or 'int4', not {kv!r}")
+        self.kv = kv if share is None else share.kv
+        self.k = self.v = self.kv4 = None
         if share is not None:
             assert share.B == B and share.max_ctx == max_ctx
-            self.k, self.v = share.k, share.v
+            self.k, self.v, self.kv4 = share.k, share.v, share.kv4
+        elif self.kv == "int4":
+            self.kv4 = [empty_kv4(B, sh.kv_heads, max_ctx, dev) for _ in range(nl)]
         else:
             cache = (B, sh.kv_heads, max_ctx, HEAD_DIM)
             self.k = [torch.zeros(cache, dtype=torch.float16, device=dev) for _ in range(nl)]
@@ -238,8 +246,25 @@ class DecoderState:
         # the last token of each sequence, for passes whose lm_head reads only it
         self.last_rows = torch.arange(B, dtype=torch.int32, device=dev) * T + (T - 1)
         self.x_last = torch.empty((B, sh.hidden), dtype=torch.float16, device=dev)
-        self.ws = torch.empty(sq_attention_workspace_bytes(B, T, sh.q_heads, sh.kv_heads, max_ctx),
-                              dtype=torch.uint8, device=dev)
+        if self.kv == "int4":
+            need = sq_attention_kv4_workspace_bytes(B, T, sh.q_heads, sh.kv_heads, kv4_ctx(max_ctx))
+        else:
+            need = sq_attention_workspace_bytes(B, T, sh.q_heads, sh.kv_heads, max_ctx)
+        self.ws = torch.empty(need, dtype=torch.uint8, device=dev)
+
+
+def kv4_ctx(max_ctx: int) -> int:
+    """Positions of a 4-bit cache that holds max_ctx: whole groups of 16."""
+    return (max_ctx + 15) // 16 * 16
+
+
+def empty_kv4(B: int, kv_heads: int, max_ctx: int, device):
+    """(k_codes, k_params, v_codes, v_params) of one layer's 4-bit cache, zeroed."""
+    C = kv4_ctx(max_ctx)
+    u8 = dict(dtype=torch.uint8, device=device)
+    f16 = dict(dtype=torch.float16, device=device)
+    return (torch.zeros((B, kv_heads, C, HEAD_DIM // 2), **u8), torch.zeros((B, kv_heads, C, 2), **f16),
+            torch.zeros((B, kv_heads, C // 2, HEAD_DIM), **u8), torch.zeros((B, kv_heads, C, 2), **f16))
 
 
 def decoder_pass(stack: LinearStack, variant: str, st: DecoderState, stream=None,
@@ -256,9 +281,10 @@ def decoder_pass(stack: LinearStack, variant: str, st: DecoderState, stream=None
     it (sq_linear_norm) and, for one new token per sequence, the cache
     append inside the attention (sq_attention_append): six launches per
     layer instead of nine; the results are bit-identical either way
-    (fuse_norm / fuse_append override the two choices)."""
-    from . import (SQ_EPI_RESIDUAL, sq_attention, sq_attention_append, sq_embed, sq_kv_append,
-                   sq_linear_norm, sq_rmsnorm)
+    (fuse_norm / fuse_append override the two choices).  A state with 4-bit
+    caches appends and attends by sq_kv4_append and sq_attention_kv4."""
+    from . import (SQ_EPI_RESIDUAL, sq_attention, sq_attention_append, sq_attention_kv4, sq_embed, sq_kv4_append,
+                   sq_kv_append, sq_linear_norm, sq_rmsnorm)
     sh = stack.shape
     wk = WKIND[variant]
     B, T = st.B, st.T
@@ -280,7 +306,11 @@ def decoder_pass(stack: LinearStack, variant: str, st: DecoderState, stream=None
     for li, (qkv, o, gu, down) in enumerate(stack.layers):
         w, s = qkv.weight(variant)
         normed(st.x, st.gamma[2 * li], st.h, w, s, SQ_EPI_NONE, st.qkv)
-        if fuse_append:
+        if st.kv4 is not None:
+            sq_kv4_append(st.qkv, sh.q_heads, sh.kv_heads, pos, ROPE_THETA, *st.kv4[li], stream=stream)
+            sq_attention_kv4(st.qkv, B, T, sh.q_heads, sh.kv_heads, pos, ROPE_THETA, *st.kv4[li], st.attn, st.ws,
+                             stream)
+        elif fuse_append:
             sq_attention_append(st.qkv, B, T, sh.q_heads, sh.kv_heads, pos, ROPE_THETA, st.k[li], st.v[li],
                                 st.attn, st.ws, stream)
         else:
@@ -301,3 +331,79 @@ def decoder_pass(stack: LinearStack, variant: str, st: DecoderState, stream=None
         x, h = st.x_last, st.h[:B]
     w, s = stack.lm_head.weight(variant)
     normed(x, st.gamma[-1], h, w, s, SQ_EPI_NONE, st.logits if logits is None else logits)
+
+
+# ---- whole prompts ------------------------------------------------------------------
+
+# Rows of one linear call (sq_linear_ex): B sequences x T tokens of a pass.
+LINEAR_MAX_ROWS = 256
+
+
+class PromptState:
+    """Activations of a pass over packed prompts: up to `rows` tokens of B
+    sequences of different lengths (offsets int32 [B+1], positions pos0 int32
+    [B], both on the device)."""
+
+    def __init__(self, stack: LinearStack, rows: int, B: int, max_ctx: int, logit_rows: int = 0):
+        from . import sq_attention_prompt_workspace_bytes
+        sh, dev = stack.shape, stack.device
+        self.rows, self.B, self.max_ctx = rows, B, max_ctx
+        f16 = dict(dtype=torch.float16, device=dev)
+        part = min(rows, LINEAR_MAX_ROWS)
+        self.x = torch.zeros((rows, sh.hidden), **f16)
+        self.h = torch.empty((part, sh.hidden), **f16)
+        self.qkv = torch.empty((rows, sh.q_out + 2 * sh.kv_out), **f16)
+        # (rows of no sequence are read by the projection behind the attention, and written by no one)
+        self.attn = torch.zeros((rows, sh.q_out), **f16)
+        self.g = torch.empty((part, sh.intermediate), **f16)
+        self.logits = torch.empty((logit_rows, sh.vocab), **f16) if logit_rows else None
+        self.x_rows = torch.empty((logit_rows, sh.hidden), **f16) if logit_rows else None
+        self.offsets = torch.zeros((B + 1,), dtype=torch.int32, device=dev)
+        self.pos0 = torch.zeros((B,), dtype=torch.int32, device=dev)
+        self.ws = torch.empty(sq_attention_prompt_workspace_bytes(B, rows, sh.q_heads, sh.kv_heads, max_ctx),
+                              dtype=torch.uint8, device=dev)
+
+
+def prompt_pass(stack: LinearStack, variant: str, st: PromptState, cache: DecoderState, stream=None,
+                scratch=None, logit_rows=None) -> None:
+    """One pass of the model over the packed prompts in st.x (embedded tokens):
+    the caches of `cache` are filled, and with logit_rows (int32, device: rows
+    of st.x, at most the state's logit_rows) the lm_head runs on those rows into
+    st.logits.  The linear layers take 256 rows a call, the attention the whole
+    batch (sq_attention_prompt).  4-bit caches: attention over fp16 keys and
+    values in `scratch` = (k, v) fp16 [B, Hkv, max_ctx, 128], shared by the
+    layers, which sq_kv4_append then keeps in 4 bits (prompts from position 0:
+    the scratch holds no earlier prefix)."""
+    from . import SQ_EPI_RESIDUAL, sq_attention_prompt, sq_embed, sq_kv4_append, sq_linear_norm
+    sh = stack.shape
+    wk = WKIND[variant]
+    heads = (sh.q_heads, sh.kv_heads)
+    parts = [slice(i, min(i + LINEAR_MAX_ROWS, st.rows)) for i in range(0, st.rows, LINEAR_MAX_ROWS)]
+
+    def normed(x, gamma, proj, epi, y):
+        w, s = proj.weight(variant)
+        sq_linear_norm(wk, x, gamma, RMS_EPS, st.h[:x.shape[0]], w, s, None, None, epi, y, stream)
+
+    def residual(a, proj, x):
+        w, s = proj.weight(variant)
+        sq_linear_ex(wk, a, w, s, None, x, SQ_EPI_RESIDUAL, x, stream)
+
+    for li, (qkv, o, gu, down) in enumerate(stack.layers):
+        for p in parts:
+            normed(st.x[p], cache.gamma[2 * li], qkv, SQ_EPI_NONE, st.qkv[p])
+        k, v = scratch if cache.kv4 is not None else (cache.k[li], cache.v[li])
+        sq_attention_prompt(st.qkv, st.offsets, *heads, st.pos0, ROPE_THETA, k, v, st.attn, st.ws, stream)
+        if cache.kv4 is not None:
+            sq_kv4_append(st.qkv, *heads, st.pos0, ROPE_THETA, *cache.kv4[li], offsets=st.offsets, stream=stream)
+        for p in parts:
+            residual(st.attn[p], o, st.x[p])
+            g = st.g[:p.stop - p.start]
+            normed(st.x[p], cache.gamma[2 * li + 1], gu, SQ_EPI_SILU_GATE, g)
+            residual(g, down, st.x[p])
+    if logit_rows is None:
+        return
+    n = logit_rows.shape[0]
+    sq_embed(logit_rows, st.x, st.x_rows[:n], stream)  # row gather
+    for i in range(0, n, LINEAR_MAX_ROWS):
+        e = min(i + LINEAR_MAX_ROWS, n)
+        normed(st.x_rows[i:e], cache.gamma[-1], stack.lm_head, SQ_EPI_NONE, st.logits[i:e])
