@@ -212,18 +212,21 @@ struct KV4AttnArgs {
 };
 
 constexpr int kK4Warps = 4, kK4Threads = 32 * kK4Warps;
-constexpr int kK4Keys = 16;                   // keys of a warp's step
-constexpr int kK4Stages = 4;                  // steps in flight a warp
+constexpr int kK4Keys = 32;                   // keys of a warp's step
+constexpr int kK4Stages = 3;                  // steps in flight a warp
 constexpr int kK4Codes = kK4Keys * 64;        // bytes of a step's key (value) codes
 constexpr int kK4Stage = 2 * kK4Codes + 2 * kK4Keys * 4;
 constexpr int kK4Rec = kAttnPartStride;       // floats of a query's partial result
-constexpr int kK4OffQ = 0;                    // queries, two fp16 terms: [2][8][128]
-constexpr int kK4OffFac = kK4OffQ + 2 * 8 * kHeadDim * 2;  // their factors and sums
-constexpr int kK4OffRing = kK4OffFac + 64;
-constexpr int kK4OffRec = kK4OffRing;         // the records, over the ring: one a warp, then the CTA's
-constexpr int kK4Smem = kK4OffRing + (kK4Warps * kK4Stages * kK4Stage > (kK4Warps + 1) * 8 * kK4Rec * 4
-                                          ? kK4Warps * kK4Stages * kK4Stage
-                                          : (kK4Warps + 1) * 8 * kK4Rec * 4);
+template <int R>
+struct K4Cfg {
+  static constexpr int kQ = 8 * R;            // queries of a CTA
+  static constexpr int kOffQ = 0;             // their operands: [R][8 k-steps][32 lanes] 16 bytes
+  static constexpr int kOffFac = R * 4096;    // their factors and sums
+  static constexpr int kOffRing = kOffFac + 8 * kQ;
+  static constexpr int kRing = kK4Warps * kK4Stages * kK4Stage;
+  static constexpr int kRecs = (kK4Warps + 1) * kQ * kK4Rec * 4;  // over the ring: one a warp, then the CTA's
+  static constexpr int kSmem = kOffRing + (kRing > kRecs ? kRing : kRecs);
+};
 
 __device__ __forceinline__ void k4_mma(float d[4], const uint32_t a[4], uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
@@ -273,29 +276,35 @@ __device__ __forceinline__ void k4_cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// One CTA: eight queries (q = g T + t) of a (sequence, key/value head) against a
-// share of its keys, four warps taking steps of 16 keys in turn.
+// One CTA: 8 R queries (q = g T + t) of a (sequence, key/value head) against a
+// share of its keys, four warps taking steps of 32 keys in turn.
 //
-// A step's codes are 2 KB that lie as the products want them: a lane copies
-// (cp.async, four steps ahead, no barrier) and reads 16 bytes of a key's row and
+// A step's codes are 4 KB that lie as the products want them: a lane copies
+// (cp.async, two steps ahead, no barrier) and reads 16 bytes of a key's row and
 // 16 of two positions' values, and every word of them becomes operands of
 // mma.m16n8k16 in the lane itself: keys as the columns of Q K^T in an order of
 // dimensions that the queries share, values as the columns of P V with positions
 // in pairs, so nothing is moved between lanes or through shared memory.  Scale
-// and lowest value of a row enter beside the products.  Queries and weights are
-// two fp16 terms each (rows 0..7 and 8..15 of a tile): nothing held in 32 bits is
-// rounded to 16.  The running maximum may lag by 2^5 before sums are rescaled, and
-// so may the power of two that brings weights times value scales into fp16's
-// range.  Bound: the codes' bytes at one token of up to eight heads a group (about
-// 230 instructions a step against 370 issue slots in the bytes' time), the products
-// for more queries, which read the same codes again out of L2.
+// and lowest value of a row enter beside the products.  Codes are 64 + n there;
+// 71.5 is taken off the sums, so that a weight's rounding meets values around
+// zero.  R = 1, up to eight queries: queries and weights are two fp16 terms each
+// (rows 0..7 and 8..15 of a tile), nothing held in 32 bits is rounded to 16.
+// R = 2: sixteen queries, rows of their own; queries are two terms (two products),
+// a weight relative to its row's maximum is rounded to fp16 (as in
+// sq_attention_prompt: with a second term half of the products would be its).
+// The running maximum may lag by 2^5 before sums are rescaled, and so may the
+// power of two that brings weights times value scales into fp16's range.
+// Bound: latency and the step's instructions; two chains of products a warp in
+// flight (steps of 16 keys had one and took 1.1 us each at ten warps an SM).
+template <int R>
 __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4AttnArgs a) {
+  using C = K4Cfg<R>;
   griddep_wait();
   griddep_launch_dependents();
   extern __shared__ __align__(128) uint8_t k4_smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
   const int bh = (int)(blockIdx.x / (unsigned)a.nsplit), split = (int)(blockIdx.x - (unsigned)bh * a.nsplit);
-  const int b = bh / a.Hkv, kvh = bh - b * a.Hkv, q0 = blockIdx.y * 8, T = a.T;
+  const int b = bh / a.Hkv, kvh = bh - b * a.Hkv, q0 = blockIdx.y * C::kQ, T = a.T;
   const int64_t p0l = a.pos0[b];
   const bool valid = p0l >= 0 && p0l + T <= a.max_ctx;
   if (!valid && split == 0 && blockIdx.y == 0 && tid == 0) atomicOr(&g_kv4_status, SQ_DEV_BAD_POSITION);
@@ -303,23 +312,27 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
   const int steps = (len + kK4Keys - 1) / kK4Keys;
   const int s0 = (int)((int64_t)split * steps / a.nsplit), s1 = (int)((int64_t)(split + 1) * steps / a.nsplit);
 
-  // this warp's ring; lane pieces of a step: keys 0..7 and 8..15, values likewise
-  const uint32_t ring = smem_u32(k4_smem) + kK4OffRing + warp * (kK4Stages * kK4Stage);
-  const uint8_t* slot0 = k4_smem + kK4OffRing + warp * (kK4Stages * kK4Stage);
+  // this warp's ring; lane pieces of eight keys: 16 bytes of a row each
+  const uint32_t ring = smem_u32(k4_smem) + C::kOffRing + warp * (kK4Stages * kK4Stage);
+  const uint8_t* slot0 = k4_smem + C::kOffRing + warp * (kK4Stages * kK4Stage);
   const int64_t row = (int64_t)bh * a.max_ctx;
+  const uint8_t* kcodes = a.c.kc + row * 64 + lane * 16;
+  const uint8_t* vcodes = a.c.vc + row * 64 + t4 * 128 + g * 16;
+  const uint8_t* params = reinterpret_cast<const uint8_t*>((lane < 8 ? a.c.kp : a.c.vp) + row * 2) + (lane & 7) * 16;
   auto request = [&](int step, int stage) {
     if (step < s1) {
-      const int64_t key = row + (int64_t)step * kK4Keys;
+      const int key = step * kK4Keys;
       const uint32_t dst = ring + stage * kK4Stage + lane * 16;
-      const uint8_t* ks = a.c.kc + key * 64 + lane * 16;
-      const uint8_t* vs = a.c.vc + key * 64 + t4 * 128 + g * 16;
-      k4_cp16(dst, ks);
-      k4_cp16(dst + 512, ks + 512);
-      k4_cp16(dst + kK4Codes, vs);
-      k4_cp16(dst + kK4Codes + 512, vs + 512);
-      if (lane < 8)  // parameters: 64 bytes of keys, 64 of values
-        k4_cp16(ring + stage * kK4Stage + 2 * kK4Codes + lane * 16,
-                reinterpret_cast<const uint8_t*>((lane < 4 ? a.c.kp : a.c.vp) + key * 2) + (lane & 3) * 16);
+      // (the cache holds whole groups of 16 keys: the second may lie past its end)
+      const int groups = key + 16 < len ? 4 : 2;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i < groups) {
+          k4_cp16(dst + i * 512, kcodes + (int64_t)key * 64 + i * 512);
+          k4_cp16(dst + kK4Codes + i * 512, vcodes + (int64_t)key * 64 + i * 512);
+        }
+      // parameters: 128 bytes of keys, 128 of values
+      if (lane < 16 && (lane & 7) < 2 * groups) k4_cp16(dst + 2 * kK4Codes, params + (int64_t)key * 4);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
@@ -327,11 +340,13 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
 #pragma unroll
   for (int i = 0; i < kK4Stages - 1; ++i) request(step + i * kK4Warps, i);
 
-  // the queries: a warp takes two, rotated in fp32, scaled by a power of two
-  __half* qs = reinterpret_cast<__half*>(k4_smem + kK4OffQ);
-  float* fac = reinterpret_cast<float*>(k4_smem + kK4OffFac);
+  // the queries: a warp takes 2 R, rotated in fp32, scaled by a power of two, as
+  // operands: k-step kk, half i of lane (g, t4): dimensions 32 t4 + 8 w + e and 4 more,
+  // w, e = i'th of (2 kk, 2 kk + 1) by words of eight codes
+  __half* qs = reinterpret_cast<__half*>(k4_smem + C::kOffQ);
+  float* fac = reinterpret_cast<float*>(k4_smem + C::kOffFac);
   if (s0 < s1)
-    for (int i = warp; i < 8; i += kK4Warps) {
+    for (int i = warp; i < C::kQ; i += kK4Warps) {
       const int q = q0 + i;
       float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // d = lane, lane + 32, lane + 64, lane + 96
       if (q < a.Q) {
@@ -354,126 +369,190 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
       for (int e = 0; e < 4; ++e) {
         __half hi, lo;
         k4_split(v[e] * up, hi, lo);
-        qs[i * kHeadDim + lane + 32 * e] = hi;
-        qs[(8 + i) * kHeadDim + lane + 32 * e] = lo;
         sum += __half2float(hi) + __half2float(lo);
+        // dimension d = lane + 32 e: t4 = e, w = lane / 8, nibble lane % 8; the pair is nibbles n, n + 4
+        const int nib = lane & 7, at = 4 * (lane >> 3) + (nib & 3), kk = at >> 1, half = at & 1;
+        // R = 1: tile rows i (high terms) and i + 8 (low); R = 2: row i of the tile of each term
+        const int ln = ((R == 1 ? i : i & 7) << 2) + e, up8 = R == 1 ? 0 : i >> 3;
+        __half* hi_at = qs + ((kk * 32 + ln) * 4 + 2 * half + up8) * 2 + (nib >> 2);
+        __half* lo_at = R == 1 ? qs + ((kk * 32 + ln) * 4 + 2 * half + 1) * 2 + (nib >> 2) : hi_at + 2048;
+        *hi_at = hi;
+        *lo_at = lo;
       }
       sum = warp_sum(sum);
       if (lane == 0) {
         // scores in units of log 2
         fac[i] = 0.08838834764831845f * 1.4426950408889634f * __uint_as_float((uint32_t)(127 + ex - 10) << 23);
-        fac[8 + i] = sum;
+        fac[C::kQ + i] = sum;
       }
     }
   __syncthreads();
-  uint32_t qa[8][4];
-  float fq = 0.0f, qsum = 0.0f;
-  if (s0 < s1) {
+  float fq[R], qsum[R];
+  int lim[R];  // the last position a row sees
+  const uint4* qop = reinterpret_cast<const uint4*>(k4_smem + C::kOffQ) + lane;
 #pragma unroll
-    for (int kk = 0; kk < 8; ++kk)
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int i = 2 * kk + half, d = 32 * t4 + 8 * (i >> 2) + (i & 3);
-        qa[kk][2 * half] = k4_pack(qs[g * kHeadDim + d], qs[g * kHeadDim + d + 4]);
-        qa[kk][2 * half + 1] = k4_pack(qs[(8 + g) * kHeadDim + d], qs[(8 + g) * kHeadDim + d + 4]);
-      }
-    fq = fac[g];
-    qsum = fac[8 + g];
+  for (int r = 0; r < R; ++r) {
+    fq[r] = s0 < s1 ? fac[8 * r + g] : 0.0f;
+    qsum[r] = s0 < s1 ? fac[C::kQ + 8 * r + g] : 0.0f;
+    lim[r] = p0 + (q0 + 8 * r + g) % T;
   }
-  const int lim = p0 + (q0 + g) % T;  // the last position this lane's query sees
 
-  float o[16][4], m = -INFINITY, l = 0.0f, zl = 0.0f, zw = 0.0f;
+  float o[16][4], m[R], l[R], zl[R], zw[R];
   float vcap = 0.0f, vup = 1.0f;  // value scales up to vcap; vup brings them to 2^9
 #pragma unroll
   for (int i = 0; i < 16; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    m[r] = -INFINITY;
+    l[r] = zl[r] = zw[r] = 0.0f;
+  }
 
   for (int it = 0; step < s1; ++it, step += kK4Warps) {
     asm volatile("cp.async.wait_group %0;" ::"n"(kK4Stages - 2) : "memory");
     __syncwarp();  // the parameters are other lanes' copies
     const uint8_t* sl = slot0 + (it % kK4Stages) * kK4Stage;
-    float sc[2][2], ws[2][2], wl[2][2];
     const bool edge = (step + 1) * kK4Keys > p0 + 1;
-    float mx = -INFINITY, vm = 0.0f;
+    float sc[R][4][2], mx[R], vm = 0.0f;
+    {
+      // scores: four columns' tiles of eight keys, two chains of products at a time
+      float s[4][4];
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      const uint4 kw = *reinterpret_cast<const uint4*>(sl + n * 512 + lane * 16);
-      const uint32_t w[4] = {kw.x, kw.y, kw.z, kw.w};
-      float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      for (int n = 0; n < 4; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t r[4];
-        k4_codes(w[i], r);
-        k4_mma(s, qa[2 * i], r[0], r[1]);
-        k4_mma(s, qa[2 * i + 1], r[2], r[3]);
+      for (int np = 0; np < 4; np += 2) {
+        const uint4 ka = *reinterpret_cast<const uint4*>(sl + np * 512 + lane * 16);
+        const uint4 kb = *reinterpret_cast<const uint4*>(sl + np * 512 + 512 + lane * 16);
+        const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t ra[4], rb[4];
+          k4_codes(wa[i], ra);
+          k4_codes(wb[i], rb);
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int term = 0; term < R; ++term) {
+              const uint4 qv = qop[(term * 8 + 2 * i + half) * 32];
+              const uint32_t qa[4] = {qv.x, qv.y, qv.z, qv.w};
+              k4_mma(s[np], qa, ra[2 * half], ra[2 * half + 1]);
+              k4_mma(s[np + 1], qa, rb[2 * half], rb[2 * half + 1]);
+            }
+        }
       }
-      const uint2 kp = *reinterpret_cast<const uint2*>(sl + 2 * kK4Codes + n * 32 + t4 * 8);
-      const uint2 vp = *reinterpret_cast<const uint2*>(sl + 2 * kK4Codes + 64 + n * 32 + t4 * 8);
+#pragma unroll
+      for (int r = 0; r < R; ++r) mx[r] = -INFINITY;
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const uint2 kp = *reinterpret_cast<const uint2*>(sl + 2 * kK4Codes + n * 32 + t4 * 8);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float2 k2 = __half22float2(*reinterpret_cast<const __half2*>(e ? &kp.y : &kp.x));
+          const float k0 = fmaf(-64.0f, k2.x, k2.y);
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            const float raw = R == 1 ? s[n][e] + s[n][e + 2] : s[n][2 * r + e];
+            float x = fq[r] * fmaf(k2.x, raw, k0 * qsum[r]);
+            if (edge && step * kK4Keys + 8 * n + 2 * t4 + e > lim[r]) x = -INFINITY;
+            sc[r][n][e] = x;
+            mx[r] = fmaxf(mx[r], x);
+          }
+        }
+      }
+    }
+    float ws[4][2], wl[4][2];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const uint2 vp = *reinterpret_cast<const uint2*>(sl + 2 * kK4Codes + 128 + n * 32 + t4 * 8);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const float2 k2 = __half22float2(*reinterpret_cast<const __half2*>(e ? &kp.y : &kp.x));
         const float2 v2 = __half22float2(*reinterpret_cast<const __half2*>(e ? &vp.y : &vp.x));
-        sc[n][e] = fq * fmaf(k2.x, s[e] + s[e + 2], fmaf(-64.0f, k2.x, k2.y) * qsum);
         ws[n][e] = v2.x;
-        wl[n][e] = v2.y;
-        if (edge && step * kK4Keys + 8 * n + 2 * t4 + e > lim) {
-          sc[n][e] = -INFINITY;
-          ws[n][e] = wl[n][e] = 0.0f;
-        }
-        mx = fmaxf(mx, sc[n][e]);
+        wl[n][e] = fmaf(7.5f, v2.x, v2.y);
+        // rows past the last token (they may hold anything) count for no query
+        if (edge && step * kK4Keys + 8 * n + 2 * t4 + e >= len) ws[n][e] = wl[n][e] = 0.0f;
         vm = fmaxf(vm, ws[n][e]);
       }
     }
-    if (__any_sync(0xffffffffu, mx - m > 5.0f || vm > vcap)) {
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+    bool grown = vm > vcap;
+#pragma unroll
+    for (int r = 0; r < R; ++r) grown = grown || mx[r] - m[r] > 5.0f;
+    if (__any_sync(0xffffffffu, grown)) {
+      float fv = 1.0f;
       vm = warp_max(vm);
-      const float mn = fmaxf(m, mx);
-      float f = m == -INFINITY ? 0.0f : k4_ex2(m - mn), fv = 1.0f;
-      m = mn;
       if (vm > vcap) {
-        // the power of two above vm becomes 1/32: weights up to 2^5 stay below 2^15
+        // the power of two above vm becomes 2^9: weights up to 2^5 stay below 2^15
         const float cap = __uint_as_float(((__float_as_uint(vm) >> 23) + 1) << 23);
         const float up = 512.0f / cap;
         fv = up / vup;
         vcap = cap;
         vup = up;
       }
-      l *= f;
-      zl *= f;
-      f *= fv;
-      zw *= f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
+      for (int r = 0; r < R; ++r) {
+        mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 1));
+        mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 2));
+        const float mn = fmaxf(m[r], mx[r]);
+        float f = m[r] == -INFINITY ? 0.0f : k4_ex2(m[r] - mn);
+        m[r] = mn;
+        l[r] *= f;
+        zl[r] *= f;
+        f *= fv;
+        zw[r] *= f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[i][e] *= f;
-    }
-    const float mm = m == -INFINITY ? 0.0f : m;
-    uint32_t pa[4];
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      __half hi[2], lo[2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float p = k4_ex2(sc[n][e] - mm);
-        l += p;
-        zl = fmaf(p, wl[n][e], zl);
-        const float x = p * (ws[n][e] * vup);
-        k4_split(x, hi[e], lo[e]);
-        zw += x;
+        for (int i = 0; i < 16; ++i) {
+          o[i][2 * r] *= f;
+          o[i][2 * r + 1] *= f;
+          if (R == 1) {
+            o[i][2] *= f;
+            o[i][3] *= f;
+          }
+        }
       }
-      pa[2 * n] = k4_pack(hi[0], hi[1]);
-      pa[2 * n + 1] = k4_pack(lo[0], lo[1]);
     }
-    const uint4 va = *reinterpret_cast<const uint4*>(sl + kK4Codes + lane * 16);
-    const uint4 vb = *reinterpret_cast<const uint4*>(sl + kK4Codes + 512 + lane * 16);
-    const uint32_t wa[4] = {va.x, va.y, va.z, va.w}, wb[4] = {vb.x, vb.y, vb.z, vb.w};
+    uint32_t pa[2][4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      uint32_t ra[4], rb[4];
-      k4_codes(wa[u], ra);
-      k4_codes(wb[u], rb);
+    for (int r = 0; r < R; ++r) {
+      const float mm = m[r] == -INFINITY ? 0.0f : m[r];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) k4_mma(o[4 * u + e], pa, ra[e], rb[e]);
+      for (int n = 0; n < 4; ++n) {
+        __half hi[2], lo[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float p = k4_ex2(sc[r][n][e] - mm);
+          l[r] += p;
+          // (a hidden row's scale may be NaN where its weight is zero)
+          const bool hidden = edge && sc[r][n][e] == -INFINITY;
+          const float x = hidden ? 0.0f : p * (ws[n][e] * vup);
+          zl[r] = hidden ? zl[r] : fmaf(p, wl[n][e], zl[r]);
+          if (R == 1) {
+            k4_split(x, hi[e], lo[e]);
+            zw[r] += x;
+          } else {
+            hi[e] = __float2half_rn(x);
+            zw[r] += __half2float(hi[e]);  // as it enters the product
+          }
+        }
+        if (R == 1) {
+          pa[n >> 1][2 * (n & 1)] = k4_pack(hi[0], hi[1]);
+          pa[n >> 1][2 * (n & 1) + 1] = k4_pack(lo[0], lo[1]);
+        } else {
+          pa[n >> 1][2 * (n & 1) + r] = k4_pack(hi[0], hi[1]);
+        }
+      }
+    }
+#pragma unroll
+    for (int np = 0; np < 2; ++np) {
+      const uint4 va = *reinterpret_cast<const uint4*>(sl + kK4Codes + np * 1024 + lane * 16);
+      const uint4 vb = *reinterpret_cast<const uint4*>(sl + kK4Codes + np * 1024 + 512 + lane * 16);
+      const uint32_t wa[4] = {va.x, va.y, va.z, va.w}, wb[4] = {vb.x, vb.y, vb.z, vb.w};
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        uint32_t ra[4], rb[4];
+        k4_codes(wa[u], ra);
+        k4_codes(wb[u], rb);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) k4_mma(o[4 * u + e], pa[np], ra[e], rb[e]);
+      }
     }
     __syncwarp();  // every lane has read the parameters
     request(step + (kK4Stages - 1) * kK4Warps, (it + kK4Stages - 1) % kK4Stages);
@@ -482,44 +561,46 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
   __syncthreads();
 
   // ---- records (m, l, -, -, o[D]) over the ring: a warp's, then the CTA's
-  float* rec = reinterpret_cast<float*>(k4_smem + kK4OffRec);
-  {
+  float* rec = reinterpret_cast<float*>(k4_smem + C::kOffRing);
+  const float down = 1.0f / vup;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
 #pragma unroll
     for (int i = 1; i < 4; i <<= 1) {
-      l += __shfl_xor_sync(0xffffffffu, l, i);
-      zl += __shfl_xor_sync(0xffffffffu, zl, i);
-      zw += __shfl_xor_sync(0xffffffffu, zw, i);
+      l[r] += __shfl_xor_sync(0xffffffffu, l[r], i);
+      zl[r] += __shfl_xor_sync(0xffffffffu, zl[r], i);
+      zw[r] += __shfl_xor_sync(0xffffffffu, zw[r], i);
     }
-    float* r = rec + (warp * 8 + g) * kK4Rec;
+    float* to = rec + (warp * C::kQ + 8 * r + g) * kK4Rec;
     if (t4 == 0) {
-      r[0] = m * 0.6931471805599453f;  // (natural units, as attention_combine_kernel has them)
-      r[1] = l;
+      to[0] = m[r] * 0.6931471805599453f;  // (natural units, as attention_combine_kernel has them)
+      to[1] = l[r];
     }
-    const float down = 1.0f / vup;
 #pragma unroll
     for (int u = 0; u < 4; ++u)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        float4 x;
-        x.x = fmaf(o[4 * u][e] + o[4 * u][e + 2] - 64.0f * zw, down, zl);
-        x.y = fmaf(o[4 * u + 1][e] + o[4 * u + 1][e + 2] - 64.0f * zw, down, zl);
-        x.z = fmaf(o[4 * u + 2][e] + o[4 * u + 2][e + 2] - 64.0f * zw, down, zl);
-        x.w = fmaf(o[4 * u + 3][e] + o[4 * u + 3][e + 2] - 64.0f * zw, down, zl);
-        *reinterpret_cast<float4*>(r + 4 + 16 * (2 * t4 + e) + 4 * u) = x;
+        float x[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float* t = o[4 * u + k];
+          x[k] = fmaf((R == 1 ? t[e] + t[e + 2] : t[2 * r + e]) - 71.5f * zw[r], down, zl[r]);
+        }
+        *reinterpret_cast<float4*>(to + 4 + 16 * (2 * t4 + e) + 4 * u) = make_float4(x[0], x[1], x[2], x[3]);
       }
   }
   __syncthreads();
-  const int nq = min(8, a.Q - q0);
-  float* mine = rec + kK4Warps * 8 * kK4Rec;
+  const int nq = min(C::kQ, a.Q - q0);
+  float* mine = rec + kK4Warps * C::kQ * kK4Rec;
   for (int i = tid; i < nq * (kHeadDim / 4); i += kK4Threads) {
     const int q = i / (kHeadDim / 4), d4 = i % (kHeadDim / 4);
     float M = -INFINITY, L = 0.0f;
     float4 O = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-    for (int w = 0; w < kK4Warps; ++w) M = fmaxf(M, rec[(w * 8 + q) * kK4Rec]);
+    for (int w = 0; w < kK4Warps; ++w) M = fmaxf(M, rec[(w * C::kQ + q) * kK4Rec]);
 #pragma unroll
     for (int w = 0; w < kK4Warps; ++w) {
-      const float* r = rec + (w * 8 + q) * kK4Rec;
+      const float* r = rec + (w * C::kQ + q) * kK4Rec;
       if (r[0] == -INFINITY) continue;
       const float f = expf(r[0] - M);
       const float4 v = *reinterpret_cast<const float4*>(r + 4 + 4 * d4);
@@ -595,7 +676,9 @@ constexpr int kK4MaxCluster = 16;
 constexpr int kK4PerSm = 3;
 
 // How many clusters of S CTAs are resident at once (cached per device).
+template <int R>
 static cudaError_t k4_resident(int S, int* n) {
+  auto k = attention_kv4_kernel<R>;
   static std::mutex mu;
   static bool ready[64] = {false};
   static int cache[64][kK4MaxCluster + 1] = {};
@@ -605,9 +688,8 @@ static cudaError_t k4_resident(int S, int* n) {
   if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   std::lock_guard<std::mutex> lock(mu);
   if (!ready[dev]) {
-    e = cudaFuncSetAttribute(attention_kv4_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kK4Smem);
-    if (e == cudaSuccess)
-      e = cudaFuncSetAttribute(attention_kv4_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, K4Cfg<R>::kSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return e;
     ready[dev] = true;
   }
@@ -615,7 +697,7 @@ static cudaError_t k4_resident(int S, int* n) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)S);
     cfg.blockDim = dim3(kK4Threads);
-    cfg.dynamicSmemBytes = kK4Smem;
+    cfg.dynamicSmemBytes = K4Cfg<R>::kSmem;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = (unsigned)S;
@@ -623,7 +705,7 @@ static cudaError_t k4_resident(int S, int* n) {
     cfg.attrs = at;
     cfg.numAttrs = 1;
     int c = 0;
-    if (cudaOccupancyMaxActiveClusters(&c, attention_kv4_kernel, &cfg) != cudaSuccess) {
+    if (cudaOccupancyMaxActiveClusters(&c, k, &cfg) != cudaSuccess) {
       (void)cudaGetLastError();
       c = 0;
     }
@@ -633,8 +715,10 @@ static cudaError_t k4_resident(int S, int* n) {
   return cudaSuccess;
 }
 
-// CTAs that share the keys of eight queries: as many as fill the SMs, at least
-// a step of 16 keys for each of a CTA's warps.
+static int k4_rows(int64_t Q) { return Q <= 8 ? 1 : 2; }
+
+// CTAs that share the keys of a group of queries: as many as fill the SMs, at
+// least a step of 32 keys for each of a CTA's warps.
 static int64_t k4_shares(int64_t groups, int64_t max_ctx) {
   const int64_t steps = (max_ctx + kK4Keys - 1) / kK4Keys;
   int64_t S = kK4PerSm * (int64_t)device_sm_count() / groups;
@@ -643,42 +727,27 @@ static int64_t k4_shares(int64_t groups, int64_t max_ctx) {
 }
 
 size_t attention_kv4_workspace_bytes(int B, int T, int Hq, int Hkv, int64_t max_ctx) {
-  const int64_t Q = (int64_t)(Hq / Hkv) * T, groups = (int64_t)B * Hkv * ((Q + 7) / 8);
+  const int64_t Q = (int64_t)(Hq / Hkv) * T, kq = 8 * k4_rows(Q), groups = (int64_t)B * Hkv * ((Q + kq - 1) / kq);
   const int64_t S = groups ? k4_shares(groups, max_ctx) : 1;
   return (S > 1 ? (size_t)(B * (int64_t)Hkv * S * Q) * kK4Rec * sizeof(float) : 0) + 16;
 }
 
 // Up to 16 shares meet in a cluster (one launch) as long as all clusters are
 // resident; a long cache under few heads takes more, which meet through the
-// workspace and a second launch, from 16 steps a warp on.
-cudaError_t launch_attention_kv4(const __half* qkv, int B, int T, int Hq, int Hkv, const int32_t* pos0,
-                                 double theta, const KV4Cache& c, int64_t max_ctx, __half* out, void* ws,
-                                 cudaStream_t st) {
-  KV4AttnArgs a = {};
-  a.qkv = qkv;
-  a.c = c;
-  a.pos0 = pos0;
-  a.out = out;
-  a.part = reinterpret_cast<float*>(ws);
-  a.B = B;
-  a.T = T;
-  a.Hq = Hq;
-  a.Hkv = Hkv;
-  a.G = Hq / Hkv;
-  a.Q = a.G * T;
-  a.max_ctx = max_ctx;
-  a.rf = rope_freq(theta);
-  const int Z = (a.Q + 7) / 8;
-  const int64_t groups = (int64_t)B * Hkv * Z;
-  int64_t S = k4_shares(groups, max_ctx);
-  a.cluster = S > 1 && (S <= kK4MaxCluster || max_ctx <= (int64_t)kK4MaxCluster * kK4Warps * kK4Keys * 16);
+// workspace and a second launch, from eight steps a warp on.
+template <int R>
+static cudaError_t launch_kv4_inst(KV4AttnArgs a, cudaStream_t st) {
+  const int Z = (a.Q + 8 * R - 1) / (8 * R);
+  const int64_t groups = (int64_t)a.B * a.Hkv * Z;
+  int64_t S = k4_shares(groups, a.max_ctx);
+  a.cluster = S > 1 && (S <= kK4MaxCluster || a.max_ctx <= (int64_t)kK4MaxCluster * kK4Warps * kK4Keys * 8);
   int n = 0;
-  cudaError_t e = k4_resident(1, &n);
+  cudaError_t e = k4_resident<R>(1, &n);
   if (e != cudaSuccess) return e;
   if (a.cluster) {
     if (S > kK4MaxCluster) S = kK4MaxCluster;
     for (; S > 1; --S) {
-      e = k4_resident((int)S, &n);
+      e = k4_resident<R>((int)S, &n);
       if (e != cudaSuccess) return e;
       if (n >= groups) break;
     }
@@ -686,9 +755,9 @@ cudaError_t launch_attention_kv4(const __half* qkv, int B, int T, int Hq, int Hk
   }
   a.nsplit = (int)S;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(S * B * Hkv), (unsigned)Z);
+  cfg.gridDim = dim3((unsigned)(S * a.B * a.Hkv), (unsigned)Z);
   cfg.blockDim = dim3(kK4Threads);
-  cfg.dynamicSmemBytes = kK4Smem;
+  cfg.dynamicSmemBytes = K4Cfg<R>::kSmem;
   cfg.stream = st;
   cudaLaunchAttribute at[2];
   int na = 0;
@@ -706,9 +775,29 @@ cudaError_t launch_attention_kv4(const __half* qkv, int B, int T, int Hq, int Hk
   }
   cfg.attrs = at;
   cfg.numAttrs = na;
-  e = cudaLaunchKernelEx(&cfg, attention_kv4_kernel, a);
+  e = cudaLaunchKernelEx(&cfg, attention_kv4_kernel<R>, a);
   if (e != cudaSuccess || a.cluster || S == 1) return e;
-  return launch_attention_combine(a.part, B, T, Hq, Hkv, a.nsplit, out, st);
+  return launch_attention_combine(a.part, a.B, a.T, a.Hq, a.Hkv, a.nsplit, a.out, st);
+}
+
+cudaError_t launch_attention_kv4(const __half* qkv, int B, int T, int Hq, int Hkv, const int32_t* pos0,
+                                 double theta, const KV4Cache& c, int64_t max_ctx, __half* out, void* ws,
+                                 cudaStream_t st) {
+  KV4AttnArgs a = {};
+  a.qkv = qkv;
+  a.c = c;
+  a.pos0 = pos0;
+  a.out = out;
+  a.part = reinterpret_cast<float*>(ws);
+  a.B = B;
+  a.T = T;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.G = Hq / Hkv;
+  a.Q = a.G * T;
+  a.max_ctx = max_ctx;
+  a.rf = rope_freq(theta);
+  return k4_rows(a.Q) == 1 ? launch_kv4_inst<1>(a, st) : launch_kv4_inst<2>(a, st);
 }
 
 cudaError_t take_kv4_status(uint32_t* bits) {
