@@ -222,7 +222,8 @@ struct K4Cfg {
   static constexpr int kQ = 8 * R;            // queries of a CTA
   static constexpr int kOffQ = 0;             // their operands: [R][8 k-steps][32 lanes] 16 bytes
   static constexpr int kOffFac = R * 4096;    // their factors and sums
-  static constexpr int kOffRing = kOffFac + 8 * kQ;
+  static constexpr int kOffCs = kOffFac + 8 * kQ;  // cos and sin of their positions
+  static constexpr int kOffRing = kOffCs + kQ * (kHeadDim / 2) * 8;
   static constexpr int kRing = kK4Warps * kK4Stages * kK4Stage;
   static constexpr int kRecs = (kK4Warps + 1) * kQ * kK4Rec * 4;  // over the ring: one a warp, then the CTA's
   static constexpr int kSmem = kOffRing + (kRing > kRecs ? kRing : kRecs);
@@ -345,6 +346,16 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
   // w, e = i'th of (2 kk, 2 kk + 1) by words of eight codes
   __half* qs = reinterpret_cast<__half*>(k4_smem + C::kOffQ);
   float* fac = reinterpret_cast<float*>(k4_smem + C::kOffFac);
+  // (a token's table once, by all threads: as many tokens as there are, or queries)
+  float2* cs = reinterpret_cast<float2*>(k4_smem + C::kOffCs);
+  const int tables = min(T, C::kQ);
+  if (s0 < s1)
+    for (int i = tid; i < tables * (kHeadDim / 2); i += kK4Threads) {
+      const int k = i / (kHeadDim / 2);
+      const RopeCS r = rope_cs_pair(p0 + (T <= C::kQ ? k : (q0 + k) % T), a.rf.f[i % (kHeadDim / 2)]);
+      cs[i] = make_float2(r.c.h, r.s.h);
+    }
+  __syncthreads();
   if (s0 < s1)
     for (int i = warp; i < C::kQ; i += kK4Warps) {
       const int q = q0 + i;
@@ -354,10 +365,10 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
         const __half* x = a.qkv + (((int64_t)b * T + t) * (a.Hq + 2 * a.Hkv) + kvh * a.G + hg) * kHeadDim + lane;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const RopeCS r = rope_cs_pair(p0 + t, a.rf.f[lane + 32 * e]);
+          const float2 r = cs[(T <= C::kQ ? t : i) * (kHeadDim / 2) + lane + 32 * e];
           const float x1 = __half2float(x[32 * e]), x2 = __half2float(x[32 * e + 64]);
-          v[e] = x1 * r.c.h - x2 * r.s.h;
-          v[e + 2] = x2 * r.c.h + x1 * r.s.h;
+          v[e] = x1 * r.x - x2 * r.y;
+          v[e + 2] = x2 * r.x + x1 * r.y;
         }
       }
       const float am = warp_max(fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3]))));
@@ -440,8 +451,6 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
         }
       }
 #pragma unroll
-      for (int r = 0; r < R; ++r) mx[r] = -INFINITY;
-#pragma unroll
       for (int n = 0; n < 4; ++n) {
         const uint2 kp = *reinterpret_cast<const uint2*>(sl + 2 * kK4Codes + n * 32 + t4 * 8);
 #pragma unroll
@@ -451,10 +460,7 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
 #pragma unroll
           for (int r = 0; r < R; ++r) {
             const float raw = R == 1 ? s[n][e] + s[n][e + 2] : s[n][2 * r + e];
-            float x = fq[r] * fmaf(k2.x, raw, k0 * qsum[r]);
-            if (edge && step * kK4Keys + 8 * n + 2 * t4 + e > lim[r]) x = -INFINITY;
-            sc[r][n][e] = x;
-            mx[r] = fmaxf(mx[r], x);
+            sc[r][n][e] = fq[r] * fmaf(k2.x, raw, k0 * qsum[r]);
           }
         }
       }
@@ -468,11 +474,30 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
         const float2 v2 = __half22float2(*reinterpret_cast<const __half2*>(e ? &vp.y : &vp.x));
         ws[n][e] = v2.x;
         wl[n][e] = fmaf(7.5f, v2.x, v2.y);
-        // rows past the last token (they may hold anything) count for no query
-        if (edge && step * kK4Keys + 8 * n + 2 * t4 + e >= len) ws[n][e] = wl[n][e] = 0.0f;
-        vm = fmaxf(vm, ws[n][e]);
       }
     }
+    if (edge) {  // rows that a query does not see, and those past the last token (they may hold anything)
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int key = step * kK4Keys + 8 * n + 2 * t4 + e;
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+            if (key > lim[r]) sc[r][n][e] = -INFINITY;
+          if (key >= len || (R == 1 && key > lim[0])) ws[n][e] = wl[n][e] = 0.0f;
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) mx[r] = -INFINITY;
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        vm = fmaxf(vm, ws[n][e]);
+#pragma unroll
+        for (int r = 0; r < R; ++r) mx[r] = fmaxf(mx[r], sc[r][n][e]);
+      }
     bool grown = vm > vcap;
 #pragma unroll
     for (int r = 0; r < R; ++r) grown = grown || mx[r] - m[r] > 5.0f;
@@ -520,12 +545,14 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
         for (int e = 0; e < 2; ++e) {
           const float p = k4_ex2(sc[r][n][e] - mm);
           l[r] += p;
-          // (a hidden row's scale may be NaN where its weight is zero)
-          const bool hidden = edge && sc[r][n][e] == -INFINITY;
-          const float x = hidden ? 0.0f : p * (ws[n][e] * vup);
-          zl[r] = hidden ? zl[r] : fmaf(p, wl[n][e], zl[r]);
+          float w = ws[n][e] * vup, wlow = wl[n][e];
+          // (a row that the one query sees and the other does not may hold a NaN)
+          if (R > 1 && edge && sc[r][n][e] == -INFINITY) w = wlow = 0.0f;
+          const float x = p * w;
+          zl[r] = fmaf(p, wlow, zl[r]);
           if (R == 1) {
-            k4_split(x, hi[e], lo[e]);
+            hi[e] = __float2half_rn(x);  // (below 2^15)
+            lo[e] = __float2half_rn(x - __half2float(hi[e]));
             zw[r] += x;
           } else {
             hi[e] = __float2half_rn(x);
