@@ -479,7 +479,9 @@ SQ_API sq_status sq_attention_prompt(const void* qkv, int64_t N, const int32_t* 
  *   writes nothing for b and sets SQ_DEV_BAD_POSITION.
  * sq_attention_kv4: sq_attention over these caches (same arguments, layouts
  *   and limits; the new tokens already appended): fp32 accumulation over
- *   exact codes, out fp16.  Rows behind a query's position have no effect,
+ *   exact codes, out fp16; above eight queries a key/value head, (Hq / Hkv) *
+ *   T > 8, a weight relative to its row's maximum is rounded to fp16 for its
+ *   product with the codes, as in sq_attention_prompt.  Rows behind a query's position have no effect,
  *   whatever they hold.  A sequence with pos0[b] < 0 or pos0[b] + T > max_ctx
  *   gets zero rows and sets SQ_DEV_BAD_POSITION.  workspace:
  *   sq_attention_kv4_workspace_bytes(...) bytes, 16-byte aligned, no

@@ -20,26 +20,21 @@ namespace sq {
 
 static __device__ unsigned int g_kv4_status;
 
-// Codes (nibble e: x[e]) of one row whose 16 lanes hold eight fp16 values each;
-// par: scale and lowest.  A quotient comes from the reciprocal (within 2^-19 of
-// the quotient: it is at most 15); only where that leaves the rounding open is
-// it divided.
-__device__ __forceinline__ uint32_t kv4_encode(const float x[8], uint32_t& par, bool& fine) {
-  float lo = x[0], hi = x[0], sum = x[0] - x[0];
+// Codes (nibble e: x[e]) of one row whose 16 lanes hold eight fp16 values each,
+// in pairs; par: scale and lowest.  Smallest and largest run through one shuffle
+// (the former negated; a NaN stays one).  A quotient comes from the reciprocal
+// (within 2^-19 of the quotient: it is at most 15); only where that leaves the
+// rounding open is it divided.
+__device__ __forceinline__ uint32_t kv4_encode(const __half2 h[4], uint32_t& par, bool& fine) {
+  const __half2 big = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
+  const __half2 small = __hmin2_nan(__hmin2_nan(h[0], h[1]), __hmin2_nan(h[2], h[3]));
+  __half2 ends = __halves2half2(__hneg(__hmin_nan(__low2half(small), __high2half(small))),
+                                __hmax_nan(__low2half(big), __high2half(big)));
 #pragma unroll
-  for (int e = 1; e < 8; ++e) {
-    lo = fminf(lo, x[e]);
-    hi = fmaxf(hi, x[e]);
-    sum += x[e] - x[e];  // (0, or NaN where one is not finite)
-  }
-#pragma unroll
-  for (int o = 8; o > 0; o >>= 1) {
-    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-    sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  }
-  fine = sum == 0.0f;
-  lo = lo == 0.0f ? 0.0f : lo;
+  for (int o = 8; o > 0; o >>= 1) ends = __hmax2_nan(ends, __shfl_xor_sync(0xffffffffu, ends, o));
+  const float2 e2 = __half22float2(ends);
+  const float lo = e2.x == 0.0f ? 0.0f : -e2.x, hi = e2.y;
+  fine = fabsf(lo) < INFINITY && fabsf(hi) < INFINITY;
   __half s16 = __float2half_rn(__fdiv_rn(__fsub_rn(hi, lo), 15.0f));
   if (__half_as_ushort(s16) == 0 && hi > lo) s16 = __ushort_as_half(1);
   const float s = __half2float(s16);
@@ -47,14 +42,20 @@ __device__ __forceinline__ uint32_t kv4_encode(const float x[8], uint32_t& par, 
   if (!fine) par = 0x7fff7fffu;  // NaN: everything read from this row is
   if (!fine || s == 0.0f) return 0;
   const float inv = __frcp_rn(s);
-  const float big = 12582912.0f;  // 1.5 2^23: its last bits count ones
+  const float one = 12582912.0f;  // 1.5 2^23: its last bits count ones
   uint32_t w = 0;
-  float open = 0.0f;
+  float x[8], open = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = __half22float2(h[i]);
+    x[2 * i] = f.x;
+    x[2 * i + 1] = f.y;
+  }
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float q = fminf(__fmul_rn(__fsub_rn(x[e], lo), inv), 15.0f);
-    const float r = __fadd_rn(q, big);
-    open = fmaxf(open, fabsf(q - (r - big)));
+    const float r = __fadd_rn(q, one);
+    open = fmaxf(open, fabsf(q - (r - one)));
     w |= (__float_as_uint(r) & 15u) << (4 * e);
   }
   if (open > 0.4999f) {
@@ -66,61 +67,51 @@ __device__ __forceinline__ uint32_t kv4_encode(const float x[8], uint32_t& par, 
   return w;
 }
 
-__device__ __forceinline__ void kv4_floats4(uint2 v, float* x) {
-  const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&v.x));
-  const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&v.y));
-  x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
-}
-
-// One CTA per R rows, which share their rotation tables; 16 lanes a (row,
-// key/value head, key or value).  A lane's eight key dimensions are 4u .. 4u + 3
-// and 64 more, its rotation entries four that lie 16 entries apart.  R = 1 while
-// that leaves no SM without a CTA, as a decode step: what counts is one row's
-// chain of operations.
+// One CTA a row (several, sharing their tables' computation, waited longer for
+// one another: 5493 rows of 8 heads, append and unpack, 35 us with four, 32 with
+// one); 16 lanes a
+// (key/value head, key or value).  A lane's eight key dimensions are 4u .. 4u + 3
+// and 64 more, its rotation entries four that lie 16 entries apart.  Bound: the
+// chain of one row (offsets, table, values, ends, codes) and, for thousands of
+// rows, instructions: about 40 a value.
 constexpr int kAppendThreads = 256;
-template <int R>
 __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(const __half* __restrict__ qkv, const Packed pk,
                                                                     int Hq, int Hkv, const RopeFreq rf,
                                                                     const KV4Cache c) {
   griddep_wait();
   griddep_launch_dependents();
-  __shared__ RopeCS cs[R][kHeadDim / 2];  // dimension d at (d % 4) * 16 + d / 4
-  __shared__ int seq[R], pos[R];
-  const int64_t row0 = (int64_t)blockIdx.x * R;
+  __shared__ RopeCS cs[kHeadDim / 2];  // dimension d at (d % 4) * 16 + d / 4
+  __shared__ int seq, pos;
+  const int64_t row = blockIdx.x;
   const int tid = threadIdx.x;
-  if (packed_rows<R>(pk, row0, seq, pos, &g_kv4_status)) return;
-  if (tid < R * (kHeadDim / 2)) {
-    const int i = tid / (kHeadDim / 2), d = tid % (kHeadDim / 2);
-    if (seq[i] >= 0 && pos[i] >= 0) cs[i][(d & 3) * 16 + (d >> 2)] = rope_cs_pair(pos[i], rf.f[d]);
-  }
+  if (packed_rows<1>(pk, row, &seq, &pos, &g_kv4_status)) return;
+  if (seq < 0 || pos < 0) return;
+  if (tid < kHeadDim / 2) cs[(tid & 3) * 16 + (tid >> 2)] = rope_cs_pair(pos, rf.f[tid]);
   __syncthreads();
   const int u = tid & 15, per = 2 * Hkv;
-  // (the lanes of a warp stay together: R 2 Hkv rows are an even number)
-  for (int j = tid >> 4; j < R * per; j += kAppendThreads / 16) {
-    const int r = R == 1 ? 0 : j / per, i = j - r * per;
-    const bool mine = seq[r] >= 0 && pos[r] >= 0;
+  // (the lanes of a warp stay together: 2 Hkv is an even number)
+  for (int i = tid >> 4; i < per; i += blockDim.x / 16) {
     const bool val = i >= Hkv;
-    const int64_t slot = mine ? ((int64_t)seq[r] * Hkv + (val ? i - Hkv : i)) * pk.max_ctx + pos[r] : 0;
-    const uint2* src =
-        reinterpret_cast<const uint2*>(qkv + ((row0 + r) * (int64_t)(Hq + per) + Hq + i) * kHeadDim);
-    float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-    if (mine) {
-      kv4_floats4(src[val ? 2 * u : u], x);
-      kv4_floats4(src[val ? 2 * u + 1 : u + 16], x + 4);
-      if (!val) {
+    const int64_t slot = ((int64_t)seq * Hkv + (val ? i - Hkv : i)) * pk.max_ctx + pos;
+    const uint2* src = reinterpret_cast<const uint2*>(qkv + (row * (Hq + per) + Hq + i) * kHeadDim);
+    const uint2 v0 = src[val ? 2 * u : u], v1 = src[val ? 2 * u + 1 : u + 16];
+    __half2 h[4];
+    h[0] = *reinterpret_cast<const __half2*>(&v0.x);
+    h[1] = *reinterpret_cast<const __half2*>(&v0.y);
+    h[2] = *reinterpret_cast<const __half2*>(&v1.x);
+    h[3] = *reinterpret_cast<const __half2*>(&v1.y);
+    if (!val) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const RopeCS t = cs[r][e * 16 + u];
-          const float a = x[e], b = x[e + 4];
-          x[e] = __half2float(rope_f16(a, t.c, -b, t.s));
-          x[e + 4] = __half2float(rope_f16(b, t.c, a, t.s));
-        }
+      for (int p = 0; p < 2; ++p) {
+        const RopeCS t0 = cs[2 * p * 16 + u], t1 = cs[(2 * p + 1) * 16 + u];
+        const float2 a = __half22float2(h[p]), b = __half22float2(h[p + 2]);
+        h[p] = __halves2half2(rope_f16(a.x, t0.c, -b.x, t0.s), rope_f16(a.y, t1.c, -b.y, t1.s));
+        h[p + 2] = __halves2half2(rope_f16(b.x, t0.c, a.x, t0.s), rope_f16(b.y, t1.c, a.y, t1.s));
       }
     }
     uint32_t par;
     bool fine;
-    const uint32_t w = kv4_encode(x, par, fine);
-    if (!mine) continue;
+    const uint32_t w = kv4_encode(h, par, fine);
     uint16_t* dst = val ? reinterpret_cast<uint16_t*>(c.vc + (slot >> 1) * kHeadDim) + (slot & 1)
                         : reinterpret_cast<uint16_t*>(c.kc + slot * (kHeadDim / 2));
     dst[val ? 4 * u : u] = (uint16_t)w;
@@ -134,12 +125,10 @@ __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(const __half
 
 cudaError_t launch_kv4_append(const __half* qkv, const Packed& pk, int Hq, int Hkv, double theta,
                               const KV4Cache& c, cudaStream_t st) {
-  constexpr int kRows = 4;
-  if (pk.N <= device_sm_count())
-    return launch_pdl(kv4_append_kernel<1>, dim3((unsigned)pk.N), dim3(kAppendThreads), 0, st, qkv, pk, Hq, Hkv,
-                      rope_freq(theta), c);
-  return launch_pdl(kv4_append_kernel<kRows>, dim3((unsigned)((pk.N + kRows - 1) / kRows)), dim3(kAppendThreads), 0,
-                    st, qkv, pk, Hq, Hkv, rope_freq(theta), c);
+  // 16 threads for each of a row's 2 Hkv parts, 64 at least for its table
+  const int threads = Hkv < 2 ? 64 : Hkv < 8 ? 32 * Hkv : kAppendThreads;
+  return launch_pdl(kv4_append_kernel, dim3((unsigned)pk.N), dim3((unsigned)threads), 0, st, qkv, pk, Hq, Hkv,
+                    rope_freq(theta), c);
 }
 
 __device__ __forceinline__ float2 kv4_params(const __half* p, int64_t slot) {
@@ -238,17 +227,6 @@ __device__ __forceinline__ void k4_mma(float d[4], const uint32_t a[4], uint32_t
 __device__ __forceinline__ void k4_cp16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
-// Eight codes to four pairs holding 64 + n: nibbles e and e + 4 of the word in
-// pair e.  A nibble in bits 4 .. 7 of an fp16 value of exponent 6 counts ones; the
-// 64 is taken off the sums (they stay within 2^-17 of exact: the products are,
-// and fp32 has 13 bits more than the result needs).
-__device__ __forceinline__ void k4_codes(uint32_t w, uint32_t r[4]) {
-  constexpr uint32_t kMask = 0x00f000f0u, kOne = 0x54005400u;
-  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r[0]) : "r"(w << 4), "r"(kMask), "r"(kOne));
-  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r[1]) : "r"(w), "r"(kMask), "r"(kOne));
-  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r[2]) : "r"(w >> 4), "r"(kMask), "r"(kOne));
-  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r[3]) : "r"(w >> 8), "r"(kMask), "r"(kOne));
-}
 __device__ __forceinline__ float k4_ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -286,9 +264,11 @@ __device__ __forceinline__ void k4_cluster_sync() {
 // mma.m16n8k16 in the lane itself: keys as the columns of Q K^T in an order of
 // dimensions that the queries share, values as the columns of P V with positions
 // in pairs, so nothing is moved between lanes or through shared memory.  Scale
-// and lowest value of a row enter beside the products.  Codes are 64 + n there;
-// 71.5 is taken off the sums, so that a weight's rounding meets values around
-// zero.  R = 1, up to eight queries: queries and weights are two fp16 terms each
+// and lowest value of a row enter beside the products.  Codes are n - 8 there, so
+// that sums stay as small as the values' own: over a long cache these cancel to a
+// hundredth of one, and an offset kept in the codes (64 + n takes two
+// instructions in nine fewer a word) left 2^-24 of itself with each addition,
+// 4 % of the result behind 30000 tokens.  R = 1, up to eight queries: queries and weights are two fp16 terms each
 // (rows 0..7 and 8..15 of a tile), nothing held in 32 bits is rounded to 16.
 // R = 2: sixteen queries, rows of their own; queries are two terms (two products),
 // a weight relative to its row's maximum is rounded to fp16 (as in
@@ -408,14 +388,14 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
     lim[r] = p0 + (q0 + 8 * r + g) % T;
   }
 
-  float o[16][4], m[R], l[R], zl[R], zw[R];
+  float o[16][4], m[R], l[R], zl[R];
   float vcap = 0.0f, vup = 1.0f;  // value scales up to vcap; vup brings them to 2^9
 #pragma unroll
   for (int i = 0; i < 16; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     m[r] = -INFINITY;
-    l[r] = zl[r] = zw[r] = 0.0f;
+    l[r] = zl[r] = 0.0f;
   }
 
   for (int it = 0; step < s1; ++it, step += kK4Warps) {
@@ -437,8 +417,8 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           uint32_t ra[4], rb[4];
-          k4_codes(wa[i], ra);
-          k4_codes(wb[i], rb);
+          int4x8_to_f16x2(wa[i], ra);
+          int4x8_to_f16x2(wb[i], rb);
 #pragma unroll
           for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -456,7 +436,7 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const float2 k2 = __half22float2(*reinterpret_cast<const __half2*>(e ? &kp.y : &kp.x));
-          const float k0 = fmaf(-64.0f, k2.x, k2.y);
+          const float k0 = fmaf(8.0f, k2.x, k2.y);
 #pragma unroll
           for (int r = 0; r < R; ++r) {
             const float raw = R == 1 ? s[n][e] + s[n][e + 2] : s[n][2 * r + e];
@@ -473,7 +453,7 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
       for (int e = 0; e < 2; ++e) {
         const float2 v2 = __half22float2(*reinterpret_cast<const __half2*>(e ? &vp.y : &vp.x));
         ws[n][e] = v2.x;
-        wl[n][e] = fmaf(7.5f, v2.x, v2.y);
+        wl[n][e] = fmaf(8.0f, v2.x, v2.y);
       }
     }
     if (edge) {  // rows that a query does not see, and those past the last token (they may hold anything)
@@ -522,7 +502,6 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
         l[r] *= f;
         zl[r] *= f;
         f *= fv;
-        zw[r] *= f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           o[i][2 * r] *= f;
@@ -553,10 +532,8 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
           if (R == 1) {
             hi[e] = __float2half_rn(x);  // (below 2^15)
             lo[e] = __float2half_rn(x - __half2float(hi[e]));
-            zw[r] += x;
           } else {
             hi[e] = __float2half_rn(x);
-            zw[r] += __half2float(hi[e]);  // as it enters the product
           }
         }
         if (R == 1) {
@@ -575,8 +552,8 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         uint32_t ra[4], rb[4];
-        k4_codes(wa[u], ra);
-        k4_codes(wb[u], rb);
+        int4x8_to_f16x2(wa[u], ra);
+        int4x8_to_f16x2(wb[u], rb);
 #pragma unroll
         for (int e = 0; e < 4; ++e) k4_mma(o[4 * u + e], pa[np], ra[e], rb[e]);
       }
@@ -596,7 +573,6 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
     for (int i = 1; i < 4; i <<= 1) {
       l[r] += __shfl_xor_sync(0xffffffffu, l[r], i);
       zl[r] += __shfl_xor_sync(0xffffffffu, zl[r], i);
-      zw[r] += __shfl_xor_sync(0xffffffffu, zw[r], i);
     }
     float* to = rec + (warp * C::kQ + 8 * r + g) * kK4Rec;
     if (t4 == 0) {
@@ -611,7 +587,7 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const float* t = o[4 * u + k];
-          x[k] = fmaf((R == 1 ? t[e] + t[e + 2] : t[2 * r + e]) - 71.5f * zw[r], down, zl[r]);
+          x[k] = fmaf(R == 1 ? t[e] + t[e + 2] : t[2 * r + e], down, zl[r]);
         }
         *reinterpret_cast<float4*>(to + 4 + 16 * (2 * t4 + e) + 4 * u) = make_float4(x[0], x[1], x[2], x[3]);
       }

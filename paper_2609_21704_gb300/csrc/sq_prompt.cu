@@ -25,7 +25,6 @@ constexpr int kPrRows = 256;    // query rows of a work item: two MMA tiles
 constexpr int kPrKeys = 128;    // keys of a block
 constexpr int kPrTile = kPrKeys * kHeadDim * 2;  // bytes of a block's keys (or values)
 constexpr int kPrK = 2, kPrV = 3;  // tiles of keys and of values in shared memory
-constexpr int kPrPrepRows = 4;  // rows of a preparing CTA
 constexpr int kPrPrepThreads = 256;
 constexpr int kPrMaxBlocks = (int)(kPromptMaxCtx / kPrKeys);
 
@@ -118,14 +117,16 @@ __device__ __forceinline__ void for_tiles(const PlanArgs& a, const PlanBatch& s,
 // turn, end together.  Few tiles (a short chunk behind a long prefix) are cut
 // along the keys: of pieces of half to twice an SM's even share of the blocks, or
 // no cut, the cheapest by rounds over the SMs x (blocks of the longest piece + 3
-// for what a piece costs besides).
-constexpr int kPlanCuts = 13;
+// for what a piece costs besides).  This CTA runs beside the ones that rotate, and
+// for short prompts it is the longest: few tiles are listed in shared memory and
+// ordered by counting, in three steps.
+constexpr int kPlanCuts = 13, kPlanTiles = 320;
 __device__ void prompt_plan(const PlanArgs& a) {
   __shared__ unsigned int start[kPrMaxBlocks + 1];
-  __shared__ unsigned long long total;
-  __shared__ unsigned int tiles, longest, pieces[kPlanCuts], piece[kPlanCuts], items, groups, recs, warp_sum_[8];
+  __shared__ unsigned int tiles, longest, total, items, groups, recs, warp_sum_[8], cost[kPlanCuts];
+  __shared__ int tile_seq[kPlanTiles], tile_row[kPlanTiles], tile_blocks[kPlanTiles];
   __shared__ PlanBatch batch;
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31;
   bool bad = false;
   for (int b = tid; b < a.pk.B; b += blockDim.x) {
     const int lo = a.pk.offsets[b], hi = a.pk.offsets[b + 1];
@@ -136,11 +137,7 @@ __device__ void prompt_plan(const PlanArgs& a) {
       batch.pos[b] = a.pk.pos0[b];
     }
   }
-  if (tid == 0) {
-    total = 0;
-    tiles = longest = items = groups = recs = 0;
-  }
-  if (tid < kPlanCuts) pieces[tid] = piece[tid] = 0;
+  if (tid == 0) tiles = longest = total = items = groups = recs = 0;
   for (int i = tid; i <= kPrMaxBlocks; i += blockDim.x) start[i] = 0;
   if (__syncthreads_or(bad)) {
     if (tid == 0) {
@@ -149,44 +146,79 @@ __device__ void prompt_plan(const PlanArgs& a) {
     }
     return;
   }
-  for_tiles(a, batch, [&](int, int, int, int, int, int blocks) {
-    atomicAdd(&total, (unsigned long long)blocks);
-    atomicAdd(&tiles, 1u);
-    atomicMax(&longest, (unsigned)blocks);
-  });
-  __syncthreads();
-  unsigned int chunk = kPrMaxBlocks + 1;
-  if ((int64_t)tiles * a.Hkv < a.max_pieces && longest > 2) {
-    const unsigned int even = (unsigned int)((total * a.Hkv + (unsigned)a.sms - 1) / (unsigned)a.sms);
-    auto cut = [&](int i) { return max(2u, (even * (4 + i) + 7) / 8); };
-    for_tiles(a, batch, [&](int, int, int, int, int, int blocks) {
-      for (int i = 0; i < kPlanCuts; ++i) {
-        const unsigned int S = ((unsigned)blocks + cut(i) - 1) / cut(i);
-        atomicAdd(&pieces[i], S);
-        atomicMax(&piece[i], ((unsigned)blocks + S - 1) / S);
-      }
-    });
-    __syncthreads();
-    // uncut: the longest tile, or the tiles in rounds of their mean
-    unsigned long long best = (unsigned long long)longest + 2;
-    const unsigned long long rounds = ((unsigned long long)tiles * a.Hkv + a.sms - 1) / a.sms;
-    if (rounds > 1) best = max(best, rounds * (total / tiles + 2));
-    for (int i = 0; i < kPlanCuts; ++i) {
-      const unsigned long long n = (unsigned long long)pieces[i] * a.Hkv;
-      const unsigned long long cost = (n + a.sms - 1) / a.sms * (piece[i] + 3);
-      if ((int64_t)n <= a.max_pieces && cost < best) {
-        best = cost;
-        chunk = cut(i);
-      }
+  for_tiles(a, batch, [&](int b, int, int, int, int row0, int blocks) {
+    const unsigned int i = atomicAdd(&tiles, 1u);
+    if (i < kPlanTiles) {
+      tile_seq[i] = b;
+      tile_row[i] = row0;
+      tile_blocks[i] = blocks;
+      atomicAdd(&total, (unsigned)blocks);  // (needed of a listed batch only)
+      atomicMax(&longest, (unsigned)blocks);
     }
-  }
-  // counting sort by the blocks of a piece
-  for_tiles(a, batch, [&](int, int, int, int, int, int blocks) {
-    const unsigned int S = ((unsigned)blocks + chunk - 1) / chunk;
-    atomicAdd(&start[((unsigned)blocks + S - 1) / S], S);
   });
   __syncthreads();
-  {
+  auto emit = [&](int b, int row0, int blocks, unsigned int S, unsigned int at) {
+    const int off = a.pk.B <= kPlanSeqs ? batch.off[b] : a.pk.offsets[b];
+    const int end = a.pk.B <= kPlanSeqs ? batch.off[b + 1] : a.pk.offsets[b + 1];
+    const int p0 = a.pk.B <= kPlanSeqs ? batch.pos[b] : a.pk.pos0[b];
+    PromptItem it = {b, off, end - off, p0, row0, 0, 0, 0, (int)S, -1, -1, 0};
+    if (S > 1) {
+      it.group = (int)atomicAdd(&groups, 1u);
+      it.rec = (int)atomicAdd(&recs, S);
+      for (int i = 0; i < 2 * a.Hkv; ++i) a.init.done[(int64_t)it.group * 2 * a.Hkv + i] = 0;
+    }
+    for (unsigned int s = 0; s < S; ++s) {
+      it.split = (int)s;
+      it.blk0 = (int)((unsigned)blocks * s / S);
+      it.blk1 = (int)((unsigned)blocks * (s + 1) / S);
+      a.init.item[at + s] = it;
+    }
+  };
+  if (tiles <= kPlanTiles) {
+    const int n = (int)tiles;
+    unsigned int chunk = kPrMaxBlocks + 1;
+    if ((int64_t)n * a.Hkv < a.max_pieces && longest > 2) {
+      const unsigned int even = (total * a.Hkv + (unsigned)a.sms - 1) / (unsigned)a.sms;
+      auto cut = [&](int i) { return max(2u, (even * (4 + i) + 7) / 8); };
+      for (int i = tid >> 5; i < kPlanCuts; i += (int)(blockDim.x >> 5)) {
+        const unsigned int c = cut(i);
+        unsigned int pieces = 0, piece = 0;
+        for (int t = lane; t < n; t += 32) {
+          const unsigned int x = (unsigned)tile_blocks[t], S = (x + c - 1) / c;
+          pieces += S;
+          piece = max(piece, (x + S - 1) / S);
+        }
+        pieces = __reduce_add_sync(0xffffffffu, pieces) * a.Hkv;
+        piece = __reduce_max_sync(0xffffffffu, piece);
+        if (lane == 0)
+          cost[i] = (int64_t)pieces > a.max_pieces ? 0xffffffffu
+                                                   : (pieces + a.sms - 1) / (unsigned)a.sms * (piece + 3);
+      }
+      __syncthreads();
+      // uncut: the longest tile, or the tiles in rounds of their mean
+      unsigned int best = longest + 2;
+      const unsigned int rounds = ((unsigned)n * a.Hkv + a.sms - 1) / (unsigned)a.sms;
+      if (rounds > 1) best = max(best, rounds * (total / (unsigned)n + 2));
+      for (int i = 0; i < kPlanCuts; ++i)
+        if (cost[i] < best) {
+          best = cost[i];
+          chunk = cut(i);
+        }
+    }
+    for (int t = tid; t < n; t += blockDim.x) {
+      const unsigned int x = (unsigned)tile_blocks[t], S = (x + chunk - 1) / chunk, piece = (x + S - 1) / S;
+      unsigned int at = 0;  // pieces of the tiles before it
+      for (int u = 0; u < n; ++u) {
+        const unsigned int y = (unsigned)tile_blocks[u], Su = (y + chunk - 1) / chunk, pu = (y + Su - 1) / Su;
+        if (pu > piece || (pu == piece && u < t)) at += Su;
+      }
+      emit(tile_seq[t], tile_row[t], (int)x, S, at);
+      atomicAdd(&items, S);
+    }
+  } else {
+    // many: a counting sort by their blocks, uncut
+    for_tiles(a, batch, [&](int, int, int, int, int, int blocks) { atomicAdd(&start[blocks], 1u); });
+    __syncthreads();
     // positions: the largest bin first
     constexpr int kPer = (kPrMaxBlocks + kPrPrepThreads) / kPrPrepThreads;
     unsigned int v[kPer], sum = 0;
@@ -200,9 +232,9 @@ __device__ void prompt_plan(const PlanArgs& a) {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const unsigned int n = __shfl_up_sync(0xffffffffu, run, o);
-      if ((tid & 31) >= o) run += n;
+      if (lane >= o) run += n;
     }
-    if ((tid & 31) == 31) warp_sum_[tid >> 5] = run;
+    if (lane == 31) warp_sum_[tid >> 5] = run;
     __syncthreads();
     run -= sum;
     for (int w = 0; w < (tid >> 5); ++w) run += warp_sum_[w];
@@ -212,24 +244,11 @@ __device__ void prompt_plan(const PlanArgs& a) {
       if (hi - i >= 0) start[hi - i] = run;
       run += v[i];
     }
+    __syncthreads();
+    for_tiles(a, batch, [&](int b, int, int, int, int row0, int blocks) {
+      emit(b, row0, blocks, 1u, atomicAdd(&start[blocks], 1u));
+    });
   }
-  __syncthreads();
-  for_tiles(a, batch, [&](int b, int off, int len, int p0, int row0, int blocks) {
-    const unsigned int S = ((unsigned)blocks + chunk - 1) / chunk;
-    const unsigned int at = atomicAdd(&start[((unsigned)blocks + S - 1) / S], S);
-    PromptItem it = {b, off, len, p0, row0, 0, 0, 0, (int)S, -1, -1, 0};
-    if (S > 1) {
-      it.group = (int)atomicAdd(&groups, 1u);
-      it.rec = (int)atomicAdd(&recs, S);
-      for (int i = 0; i < 2 * a.Hkv; ++i) a.init.done[(int64_t)it.group * 2 * a.Hkv + i] = 0;
-    }
-    for (unsigned int s = 0; s < S; ++s) {
-      it.split = (int)s;
-      it.blk0 = (int)((unsigned)blocks * s / S);
-      it.blk1 = (int)((unsigned)blocks * (s + 1) / S);
-      a.init.item[at + s] = it;
-    }
-  });
   __syncthreads();
   if (tid == 0) {
     PromptWork w = a.init;
@@ -249,12 +268,17 @@ __device__ __forceinline__ bool any_nonfinite8(uint4 v) {
   return odd;
 }
 
-// CTA 0 plans; the others take kPrPrepRows rows each: the rotated queries into
+// CTA 0 plans; the others take R rows each: the rotated queries into
 // the workspace, [Hkv, N, G, D], the rotated keys and the values into the
 // caches.  A sequence that does not fit its cache writes nothing there, and
 // zeros to its rows of `out`.  16 bytes (eight values) a thread and access, of
 // both halves of a head for the rotation; bound by these bytes for long
-// prompts (the queries are written once and read once more than they must).
+// prompts (the queries are written once and read once more than they must: 8000
+// rows of 40 / 8 heads 50 us, 4.6 TB/s).  Rows of a CTA share the look at the
+// offsets; with few of them a CTA's chain counts, with many the CTAs (call of 300
+// rows R = 1, 2, 4: 90, 92, 99 us, of 2900 47.8, 47.1, 48.8, of 8000 550, 544, 544).
+constexpr int64_t kPrFewRows = 1024;  // up to here R = 1, above 2
+template <int R>
 __global__ void __launch_bounds__(kPrPrepThreads) prompt_prepare_kernel(
     const __half* __restrict__ qkv, int Hq, const RopeFreq rf, const __grid_constant__ PlanArgs a,
     __half* __restrict__ kc, __half* __restrict__ vc, __half* __restrict__ qr, __half* __restrict__ out) {
@@ -266,12 +290,12 @@ __global__ void __launch_bounds__(kPrPrepThreads) prompt_prepare_kernel(
   }
   const Packed& pk = a.pk;
   const int G = a.G, Hkv = a.Hkv, tid = threadIdx.x;
-  __shared__ RopeCS cs[kPrPrepRows][kHeadDim / 2];
-  __shared__ float2 csq[kPrPrepRows][kHeadDim / 2];  // the heads, for queries
-  __shared__ int seq[kPrPrepRows], pos[kPrPrepRows];
-  const int64_t row0 = (int64_t)(blockIdx.x - 1) * kPrPrepRows;
-  if (packed_rows<kPrPrepRows>(pk, row0, seq, pos, &g_prompt_status)) return;
-  {
+  __shared__ RopeCS cs[R][kHeadDim / 2];
+  __shared__ float2 csq[R][kHeadDim / 2];  // the heads, for queries
+  __shared__ int seq[R], pos[R];
+  const int64_t row0 = (int64_t)(blockIdx.x - 1) * R;
+  if (packed_rows<R>(pk, row0, seq, pos, &g_prompt_status)) return;
+  if (tid < R * (kHeadDim / 2)) {
     const int i = tid / (kHeadDim / 2), d = tid % (kHeadDim / 2);
     // (eight neighbouring dimensions lie 128 bytes apart, so that the lanes of a head read neighbours)
     if (seq[i] >= 0 && pos[i] >= 0) {
@@ -283,7 +307,7 @@ __global__ void __launch_bounds__(kPrPrepThreads) prompt_prepare_kernel(
   __syncthreads();
   const int64_t width = (int64_t)(Hq + 2 * Hkv) * kHeadDim;
   const int tasks = (Hq + Hkv) * 8;
-  for (int idx = tid; idx < kPrPrepRows * tasks; idx += kPrPrepThreads) {
+  for (int idx = tid; idx < R * tasks; idx += kPrPrepThreads) {
     const int i = idx / tasks, r = idx - i * tasks, h = r >> 3, u = r & 7;
     const int64_t row = row0 + i;
     const int b = seq[i];
@@ -321,7 +345,7 @@ __global__ void __launch_bounds__(kPrPrepThreads) prompt_prepare_kernel(
     reinterpret_cast<uint4*>(dst + u * 8)[8] = y2;
   }
   // values: 16 lanes a head's row
-  for (int idx = tid; idx < kPrPrepRows * Hkv * 16; idx += kPrPrepThreads) {
+  for (int idx = tid; idx < R * Hkv * 16; idx += kPrPrepThreads) {
     const int i = idx / (Hkv * 16), r = idx - i * (Hkv * 16), h = r >> 4, u = r & 15;
     const int64_t row = row0 + i;
     const bool mine = seq[i] >= 0 && pos[i] >= 0;
@@ -962,6 +986,8 @@ __global__ void __launch_bounds__(kPrThreads, 1)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
+#undef PR_BAR
+
 // [rows, 128] fp16, or [heads, rows, 128]: boxes of 64 values x 128 rows.
 static bool prompt_map(CUtensorMap* m, const void* base, int64_t rows, int64_t heads) {
   auto enc = tensor_map_encoder();
@@ -1012,9 +1038,10 @@ cudaError_t launch_prompt(const __half* qkv, const Packed& pk, int Hq, int Hkv, 
   a.init.done = reinterpret_cast<unsigned int*>(w + l.done);
   a.init.odd = w + l.odd;
   a.init.rec = reinterpret_cast<float*>(w + l.rec);
-  const unsigned int ctas = (unsigned int)((pk.N + kPrPrepRows - 1) / kPrPrepRows) + 1;
-  e = launch_pdl(prompt_prepare_kernel, dim3(ctas), dim3(kPrPrepThreads), 0, st, qkv, Hq, rope_freq(theta), a, kc,
-                 vc, qr, out);
+  const int rows = pk.N <= kPrFewRows ? 1 : 2;
+  e = launch_pdl(rows == 1 ? prompt_prepare_kernel<1> : prompt_prepare_kernel<2>,
+                 dim3((unsigned)((pk.N + rows - 1) / rows + 1)), dim3(kPrPrepThreads), 0, st, qkv, Hq,
+                 rope_freq(theta), a, kc, vc, qr, out);
   if (e != cudaSuccess) return e;
   PromptArgs p = {a.work, vc, out, Hq, Hkv, a.G, pk.N, pk.max_ctx};
   int64_t grid = (pk.N * a.G / kPrRows + pk.B) * Hkv;

@@ -297,3 +297,25 @@ def test_offsets_beyond_32_bits():
         got = out[b * T:(b + 1) * T].float().cpu().numpy().astype(np.float64)
         # nine times the scores of normal queries and keys
         assert (np.abs(got - ref.reshape(T, -1)) <= 9 * bound.reshape(T, -1)).all()
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,ctx", [(1, 5, 1, 30000), (5, 7, 1, 30000), (1, 8, 2, 120000), (3, 16, 2, 9000)])
+def test_long_caches_keep_their_precision(T, Hq, Hkv, ctx):
+    """Over a long cache values cancel to a hundredth of one, and what is left has
+    to be right: as a whole within the root of the sum of the output's rounding
+    and a weight's (each 2^-11 / sqrt(3) at most of a uniform mantissa, 2.8e-4)
+    and half as much for fp32 sums of queries and scores."""
+    rng = np.random.default_rng(ctx + T)
+    C = (ctx + T + 15) // 16 * 16
+    cache, vals = _random_cache(rng, 1, Hkv, C, [ctx], T)
+    qkv = rng.normal(0, 1, (T, (Hq + 2 * Hkv) * D)).astype(np.float16)
+    out = torch.empty(T, Hq * D, dtype=torch.float16, device=dev())
+    _attention(qkv, 1, T, Hq, Hkv, [ctx], [_t(c) for c in cache], out)
+    assert sq.sq_check() == 0
+    pos = ctx + np.arange(T)
+    q = oracle.rope(qkv[:, :Hq * D].astype(np.float64), pos, Hq, D, THETA).reshape(T, Hq, D)
+    L = ctx + T
+    ref = oracle.attention(q, vals[0][0, :, :L].transpose(1, 0, 2), vals[1][0, :, :L].transpose(1, 0, 2), pos)
+    got = out.float().cpu().numpy().astype(np.float64)
+    rel = np.linalg.norm(got - ref.reshape(T, -1)) / np.linalg.norm(ref)
+    assert rel <= 2.8e-4 * (2 ** 0.5 + 0.5), rel

@@ -287,3 +287,31 @@ def test_same_call_same_bits():
     one = _run(*args, 40, 8)[0]
     for _ in range(3):
         assert np.array_equal(one.view(np.uint16), _run(*args, 40, 8)[0].view(np.uint16))
+
+
+def test_long_prefix_keeps_its_precision():
+    """As a whole within the root of the sum of the output's rounding and a
+    weight's (each at most 2.8e-4, 2^-11 / sqrt(3)), and half as much for fp32 sums."""
+    lens, pos0, Hq, Hkv = [9], [30000], 10, 2
+    args = _case(13, lens, pos0, Hq, Hkv, 30016)
+    got, _, _ = _run(*args, Hq, Hkv)
+    ref, _, _, _ = prompt(args[0], lens, pos0, args[1], Hq, Hkv, args[3], args[4])
+    rel = np.linalg.norm(got.astype(np.float64) - ref) / np.linalg.norm(ref)
+    assert rel <= 2.8e-4 * (2 ** 0.5 + 0.5), rel
+
+
+@pytest.mark.parametrize("B,n,G,Hkv", [(600, 3, 5, 1), (400, 20, 16, 1), (513, 1, 2, 2)])
+def test_many_sequences(B, n, G, Hkv):
+    """More sequences, and more tiles, than the plan keeps in shared memory."""
+    rng = np.random.default_rng(B)
+    lens = rng.integers(0, n + 1, B).tolist()
+    if B == 400:
+        lens = [n] * B
+    pos0 = rng.integers(0, 40, B).tolist()
+    args = _case(B, lens, pos0, G * Hkv, Hkv, 64, pad=2)
+    got, k, v = _run(*args, G * Hkv, Hkv)
+    assert sq.sq_check() == 0
+    ref, bound, rk, rv = prompt(args[0], lens, pos0, args[1], G * Hkv, Hkv, args[3], args[4])
+    assert np.array_equal(k.view(np.uint16), rk.view(np.uint16))
+    assert np.array_equal(v.view(np.uint16), rv.view(np.uint16))
+    _assert(got, ref, bound)
