@@ -552,6 +552,13 @@ __device__ __forceinline__ int pr_blocks(const PromptItem& it, int G, int h) {
 // The running maximum of a row is let lag by up to 2^kPrSlack before O and the
 // sum are rescaled (the result is the same but for fp16's range), so that O
 // leaves TMEM once, at the end.
+// Bound: the chain of a half's block (scores, softmax, weights, products), as its
+// scores have one place.  8000 tokens, 40 / 8 heads: 485 us, 1.35 PFLOP/s, the
+// tensor pipe busy for 59 % of them; 1.83 us for both halves' block, 1.06 of them
+// products.  Scores of 64 keys in two places (the next ones are there before the
+// weights are) cost 735 us for the call instead of 541: twice the hand-overs, and
+// products of 64 columns; sixteen softmax warps 554; exponentials of the first 64
+// keys before the block's maximum is known 547.
 __global__ void __launch_bounds__(kPrThreads, 1)
     prompt_attention_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk,
                             const __grid_constant__ CUtensorMap tv, const PromptArgs a) {
@@ -604,8 +611,8 @@ __global__ void __launch_bounds__(kPrThreads, 1)
     return r * (int)gridDim.x + ((r & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
   };
 
-  // registers: 384 threads x 168 at launch; the softmax groups take 216, the
-  // others keep 72 (256 x 216 + 128 x 72 = 384 x 168)
+  // registers: 384 threads x 168 at launch; the softmax groups take 208, the
+  // others keep 88 (256 x 208 + 128 x 88 = 384 x 168); with 72 those spilled
   if (warp >= 8) {
    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
    if (warp == 8) {
@@ -738,7 +745,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
       const int nb = max(pr_blocks(it, a.G, 0), pr_blocks(it, a.G, 1)), end = it.pos0 + it.len;
       // the marks of a block are read a block ahead: what a tile waits for here is
       // in the chain of every tile (with the read in it, and a fence that nothing
-      // needed: 8000 tokens 40 / 8 heads 656 us)
+      // needed, the call of 8000 tokens took 14 us more)
       auto marks = [&](int j) {
         uint32_t m = 0;
 #pragma unroll
