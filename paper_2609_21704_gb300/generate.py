@@ -30,7 +30,7 @@ import torch
 from . import (SQ_ACCEPT_GREEDY, SQ_ACCEPT_SAMPLE, sq_accept_logits, sq_accept_logits_workspace_bytes,
                sq_check, sq_embed, sq_logprobs, sq_sample_logits, sq_spec_commit, sq_spec_drafts, synth)
 from .stack import (HEAD_DIM, LINEAR_MAX_ROWS, DecoderState, LinearStack, PromptState, decoder_pass,
-                    prompt_pass)
+                    kv4_ctx, prompt_pass)
 
 # Limits of one sq_attention call (see its declaration): at most 32 new
 # tokens per sequence, and (Hq / Hkv) * T <= 200 queries per key/value head.
@@ -170,7 +170,7 @@ class Generator:
                 st = PromptState(self.stack, rows, B, self.max_ctx, logit_rows=B)
                 scratch = None
                 if self.tv.kv == "int4" or (self.d2 is not None and self.d2.kv == "int4"):
-                    shape = (B, self.stack.shape.kv_heads, self.max_ctx, HEAD_DIM)
+                    shape = (B, self.stack.shape.kv_heads, kv4_ctx(self.max_ctx), HEAD_DIM)
                     scratch = tuple(torch.zeros(shape, dtype=torch.float16, device=dev) for _ in range(2))
                 self._packed = (st, scratch)
             st, scratch = self._packed
@@ -188,11 +188,11 @@ class Generator:
             self.len.copy_(torch.tensor(lens, dtype=torch.int32))
             self._cycles = 0
             sq_embed(ids_t, self.table, st.x, stream)
-            prompt_pass(self.stack, self.verifier, st, self.tv, stream, scratch, logit_rows=last)
+            prompt_pass(self.stack, self.verifier, st, self.tv, stream, scratch, last, prefix=False)
             self.z1.copy_(st.logits)
             if self.K > 0:
                 sq_embed(ids_t, self.table, st.x, stream)
-                prompt_pass(self.stack, self.draft, st, self.d2, stream, scratch)
+                prompt_pass(self.stack, self.draft, st, self.d2, stream, scratch, prefix=False)
             self.u1.copy_(torch.from_numpy(synth.uniforms(self.seed ^ 0x9F1, (B, 1))).to(dev))
             self._pick(self.z1, self.u1, self.tok1, stream)
             sq_spec_commit(None, self.tok1, self.hist, self.len, self.pos, self.last2, self.K, stream)

@@ -360,21 +360,26 @@ class PromptState:
         self.x_rows = torch.empty((logit_rows, sh.hidden), **f16) if logit_rows else None
         self.offsets = torch.zeros((B + 1,), dtype=torch.int32, device=dev)
         self.pos0 = torch.zeros((B,), dtype=torch.int32, device=dev)
-        self.ws = torch.empty(sq_attention_prompt_workspace_bytes(B, rows, sh.q_heads, sh.kv_heads, max_ctx),
-                              dtype=torch.uint8, device=dev)
+        self.first = torch.zeros((B,), dtype=torch.int32, device=dev)
+        need = sq_attention_prompt_workspace_bytes(B, rows, sh.q_heads, sh.kv_heads, kv4_ctx(max_ctx))
+        self.ws = torch.empty(need, dtype=torch.uint8, device=dev)
 
 
 def prompt_pass(stack: LinearStack, variant: str, st: PromptState, cache: DecoderState, stream=None,
-                scratch=None, logit_rows=None) -> None:
+                scratch=None, logit_rows=None, prefix: bool = True) -> None:
     """One pass of the model over the packed prompts in st.x (embedded tokens):
     the caches of `cache` are filled, and with logit_rows (int32, device: rows
     of st.x, at most the state's logit_rows) the lm_head runs on those rows into
     st.logits.  The linear layers take 256 rows a call, the attention the whole
     batch (sq_attention_prompt).  4-bit caches: attention over fp16 keys and
-    values in `scratch` = (k, v) fp16 [B, Hkv, max_ctx, 128], shared by the
-    layers, which sq_kv4_append then keeps in 4 bits (prompts from position 0:
-    the scratch holds no earlier prefix)."""
-    from . import SQ_EPI_RESIDUAL, sq_attention_prompt, sq_embed, sq_kv4_append, sq_linear_norm
+    values in `scratch` = (k, v) fp16 [B, Hkv, kv4_ctx(max_ctx), 128], shared by
+    the layers: what the caches hold before pos0 is read back into it
+    (sq_kv4_unpack; prefix False leaves that out, for prompts that all begin at
+    position 0), and the prompts' own rows then go to 4 bits (sq_kv4_append)."""
+    from . import (SQ_EPI_RESIDUAL, sq_attention_prompt, sq_embed, sq_kv4_append, sq_kv4_unpack,
+                   sq_linear_norm)
+    if cache.kv4 is not None and scratch is None:
+        raise ValueError("a pass over 4-bit caches needs the scratch for keys and values")
     sh = stack.shape
     wk = WKIND[variant]
     heads = (sh.q_heads, sh.kv_heads)
@@ -392,6 +397,8 @@ def prompt_pass(stack: LinearStack, variant: str, st: PromptState, cache: Decode
         for p in parts:
             normed(st.x[p], cache.gamma[2 * li], qkv, SQ_EPI_NONE, st.qkv[p])
         k, v = scratch if cache.kv4 is not None else (cache.k[li], cache.v[li])
+        if cache.kv4 is not None and prefix:
+            sq_kv4_unpack(*cache.kv4[li], st.first, st.pos0, k, v, stream)
         sq_attention_prompt(st.qkv, st.offsets, *heads, st.pos0, ROPE_THETA, k, v, st.attn, st.ws, stream)
         if cache.kv4 is not None:
             sq_kv4_append(st.qkv, *heads, st.pos0, ROPE_THETA, *cache.kv4[li], offsets=st.offsets, stream=stream)

@@ -146,6 +146,56 @@ def test_a_pass_over_a_4_bit_cache_is_near_the_fp16_one(stack):
     assert 0 < diff.max() < 0.5 * logits[0].std()
 
 
+def test_prompts_behind_a_4_bit_prefix(stack):
+    """The next part of each text behind what the 4-bit caches hold: bit for bit
+    the pass over fp16 caches that hold the same rows read back.  What the
+    scratch holds besides, here NaN, has no part in it."""
+    B, C, heads = 4, 70, (TINY.q_heads, TINY.kv_heads)
+    parts = [LENS, [3, 8, 1, 6]]
+    cache = DecoderState(stack, B, 1, C, kv="int4")
+    ref = DecoderState(stack, B, 1, C, share_gains=cache)
+    shape = (B, heads[1], 80, 128)
+    scratch = tuple(torch.full(shape, float("nan"), dtype=torch.float16, device=dev()) for _ in range(2))
+
+    def run(into, lens, pos):
+        st = PromptState(stack, sum(lens), B, C)
+        st.offsets.copy_(torch.tensor(np.concatenate([[0], np.cumsum(lens)]), dtype=torch.int32))
+        st.pos0.copy_(torch.tensor(pos, dtype=torch.int32))
+        ids = torch.tensor(sum(_prompts(lens, seed=90), []), dtype=torch.int32, device=dev())
+        sq.sq_embed(ids, stack.embedding(), st.x)
+        prompt_pass(stack, "fp16", st, into, scratch=scratch if into.kv4 is not None else None)
+        return st.x
+
+    run(cache, parts[0], [0] * B)
+    first, last = torch.zeros(B, dtype=torch.int32, device=dev()), torch.tensor(parts[0], dtype=torch.int32, device=dev())
+    for li in range(len(stack.layers)):
+        back = tuple(torch.zeros(shape, dtype=torch.float16, device=dev()) for _ in range(2))
+        sq.sq_kv4_unpack(*cache.kv4[li], first, last, *back)
+        ref.k[li].copy_(back[0][:, :, :C])
+        ref.v[li].copy_(back[1][:, :, :C])
+    for t in scratch:
+        t.fill_(float("nan"))
+    got, want = run(cache, parts[1], parts[0]), run(ref, parts[1], parts[0])
+    assert sq.sq_check() == 0
+    assert torch.isfinite(want).all() and torch.equal(got, want)
+
+
+def test_4_bit_caches_of_any_length(stack, params):
+    """max_ctx that is no multiple of 16: the caches hold whole groups."""
+    prompts, s = _prompts(), torch.cuda.Stream()
+    g = Generator(stack, len(prompts), 0, max(LENS), 70, verifier_kv="int4")
+    g.prefill_packed(prompts, s)
+    g.run(5, s)
+    assert g.status() == 0
+    assert _compare(g.tokens(), params, prompts, 1) > 0
+
+
+def test_a_4_bit_pass_without_scratch_is_refused(stack):
+    cache, st = DecoderState(stack, 1, 1, 16, kv="int4"), PromptState(stack, 4, 1, 16)
+    with pytest.raises(ValueError):
+        prompt_pass(stack, "fp16", st, cache)
+
+
 def test_refusals(stack):
     s = torch.cuda.Stream()
     g = Generator(stack, 2, 1, 8, 64)
