@@ -1,5 +1,5 @@
 // sq_kv4.cu -- the key/value cache in four bits: append, read back, decode
-// attention.
+// attention (by mma.sync, and by tcgen05 for many queries over long caches).
 //
 // A row (one position of one key/value head) of 128 fp16 values x, the key
 // rotated and rounded to fp16 first, is kept as
@@ -13,8 +13,11 @@
 // one.  Values lie in pairs of positions, 128 bytes a pair: two bytes (four
 // dimensions) of the even position, then those of the odd one.
 #include "sq_packed.cuh"
+#include "sq_tcgen.cuh"
 
 #include <mutex>
+#include <stddef.h>
+#include <type_traits>
 
 namespace sq {
 
@@ -275,11 +278,11 @@ __device__ __forceinline__ void k4_cluster_sync() {
 // sq_attention_prompt: with a second term half of the products would be its).
 // The running maximum may lag by 2^5 before sums are rescaled, and so may the
 // power of two that brings weights times value scales into fp16's range.
-// Bound: the step's instructions (700, R = 2) and its products together, two
-// chains of these a warp in flight: 16 x 5 tokens behind 30000, 28 / 4 heads:
-// 281 us, issue 52 % and tensor pipe 48 % busy, and no split of the keys into 3 to
-// 9 shares instead of 2 is more than 2 % faster (steps of 16 keys: 434 us).  R = 1:
-// the chain of a CTA's few steps, 4 x 8000 keys, 40 / 8 heads 19.9 us, 1.8 TB/s.
+// Bound: the products, 96 a step (R = 2; 64 with R = 1) of 16 cycles on each quarter
+// of an SM: 456 CTAs over 30000 keys take 196 ns a step of an SM, 150 with R = 1,
+// with two CTAs an SM 213 and 162; two or four CTAs' worth of registers and 3 to 9
+// shares of the keys change the call by 2 % at most.  R = 1 over a few steps: their
+// chain, 4 x 8000 keys, 40 / 8 heads 19.9 us, 1.8 TB/s.
 template <int R>
 __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4AttnArgs a) {
   using C = K4Cfg<R>;
@@ -579,8 +582,10 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
     }
     float* to = rec + (warp * C::kQ + 8 * r + g) * kK4Rec;
     if (t4 == 0) {
-      to[0] = m[r] * 0.6931471805599453f;  // (natural units, as attention_combine_kernel has them)
-      to[1] = l[r];
+      // (natural units, as attention_combine_kernel has them, which takes sums above
+      // zero only: where weights are NaN, and so the values' sums are, the record has to count)
+      to[0] = isnan(l[r]) ? 0.0f : m[r] * 0.6931471805599453f;
+      to[1] = isnan(l[r]) ? 1.0f : l[r];
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u)
@@ -678,6 +683,591 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
   if (S > 1) k4_cluster_sync();  // no CTA leaves while another reads its records
 }
 
+// ---- many queries over long caches: tcgen05 ----------------------------------------
+
+// One CTA an SM: N queries (32 or 48) of a (sequence, key/value head) against a share
+// of its keys, in tiles of 128.  Transposed products, so that keys and dimensions
+// fill the 128 rows of the tensor core and queries are its columns:
+//   S^T = K Q^T (a key's codes a row, queries in two fp16 terms: two products),
+//   O^T += V^T P^T (a dimension's codes a row).
+// A warp copies the cache's tiles as they are (three in flight; loads into registers
+// would be waited for by the fence before every hand-over).  Two groups of four warps
+// turn the keys' and the values' codes into fp16 operands, once for all queries.
+// Four warps have a key a thread: its scale and lowest value enter beside the
+// products, its weights times its value's scale go to shared memory as fp16, and it
+// keeps sums of weights (and of weights times lowest values) for every query to the
+// end.  The queries' running maxima lie in shared memory, may lag by 2^5, and change
+// where the four warps agree.  One thread issues the products.
+// attention_kv4_kernel converts a code for every sixteen queries and is bound by
+// mma.sync, 16 cycles an m16n8k16 on each quarter of an SM: 16 x 5 tokens behind
+// 30000, 28 / 4 heads, 282 us.  Here 167, 1.3 us a tile: with neither copies,
+// conversion nor softmax it takes 140, with a third of the products besides 105: the
+// rest are hand-overs (weights written, products, their place free).  Two places for
+// the weights and two tiles of copies in flight instead of one and three: 182; one
+// group for keys and values 196; codes loaded into registers 302.
+constexpr int kT4Keys = 128, kT4Threads = 512;
+constexpr int kT4Tile = kT4Keys * kHeadDim * 2;  // fp16 operands of a tile's keys (or values)
+constexpr int kT4Max = 48;                       // queries of a CTA
+constexpr int kT4OffV = 2 * kT4Tile, kT4OffP = 4 * kT4Tile;
+constexpr int kT4P = kT4Keys * 128;              // weights of a tile: 64 queries' places a key
+constexpr int kT4OffQ = kT4OffP + kT4P;      // two terms x two halves of the dimensions
+constexpr int kT4QRows = kT4Max * 128;           // bytes of a term's half
+constexpr int kT4OffC = kT4OffQ + 4 * kT4QRows;  // tiles of the cache as it is: codes, then parameters
+constexpr int kT4Stages = 3;
+constexpr int kT4Codes = kT4Keys * 64, kT4Stage = 2 * kT4Codes + 2 * kT4Keys * 4;
+constexpr int kT4OffS = kT4OffC + kT4Stages * kT4Stage;
+struct T4Shared {
+  float m[kT4Max], fac[kT4Max];  // running maxima (units of log 2); what sums are rescaled by
+  alignas(16) float neg[kT4Max];
+  alignas(16) float qsum[kT4Max];
+  int lim[kT4Max];               // the last position a query sees
+  float wm[4][kT4Max], wv[4];    // maxima of the warps: scores, value scales
+  float total[2][kT4Max];
+  int amax;                      // largest finite |query value|, as bits
+  uint64_t c_full[kT4Stages], c_empty[kT4Stages], k_full[2], v_full[2], s_full[2], p_ready[2], pv_done[2], drain;
+  uint32_t tmem;
+  int dead;
+};
+constexpr int kT4Smem = kT4OffS + (int)sizeof(T4Shared) + 1024;
+static_assert(kT4Smem <= 227 * 1024, "fits an SM");
+
+__device__ __forceinline__ uint64_t t4_desc_mn(uint32_t saddr) {  // 64 columns a row, an atom of 8 rows 1024 on
+  uint64_t d = (uint64_t)((saddr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)(8192 >> 4) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+__device__ __forceinline__ uint32_t t4_any(uint32_t x) {  // of the 128 softmax threads
+  uint32_t r;
+  asm volatile(
+      "{\n.reg .pred p, q;\nsetp.ne.u32 p, %1, 0;\nbar.red.or.pred q, 1, 128, p;\nselp.u32 %0, 1, 0, q;\n}\n"
+      : "=r"(r)
+      : "r"(x)
+      : "memory");
+  return r;
+}
+// Where 16 bytes go: words' dimensions 8 W .. 8 W + 7 of a row, in the order 0 4 1 5 2 6
+// 3 7 of the codes' conversion.  Halves of the dimensions 64 columns each; the second
+// has its words in another order, so that eight lanes' stores meet eight bank groups.
+__device__ __forceinline__ uint32_t t4_piece(int row, int W) {
+  const int half = W >> 3, piece = (W & 4) | ((W & 3) ^ (half * 2));
+  return (uint32_t)(row * 128 + ((piece ^ (row & 7)) << 4));
+}
+
+template <int N>
+__global__ void __launch_bounds__(kT4Threads, 1) attention_kv4_tc_kernel(const KV4AttnArgs a) {
+  extern __shared__ uint8_t t4_raw[];
+  uint8_t* smem = t4_raw + (((smem_u32(t4_raw) + 1023u) & ~1023u) - smem_u32(t4_raw));
+  T4Shared* s = reinterpret_cast<T4Shared*>(smem + kT4OffS);
+  const uint32_t base = smem_u32(smem), bars = base + kT4OffS;
+#define T4_BAR(member) (bars + (uint32_t)offsetof(T4Shared, member))
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < kT4Stages; ++i) {
+      mbar_init(&s->c_full[i], 1);
+      mbar_init(&s->c_empty[i], 12);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&s->k_full[i], 4);
+      mbar_init(&s->v_full[i], 4);
+      mbar_init(&s->s_full[i], 1);
+      mbar_init(&s->p_ready[i], 4);
+      mbar_init(&s->pv_done[i], 1);
+    }
+    mbar_init(&s->drain, 1);
+    s->dead = 0;
+    s->amax = 0;
+    fence_mbar_init();
+  }
+  if (warp == 12) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s->tmem)),
+                 "r"(256)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *(volatile uint32_t*)&s->tmem;  // S^T at 0 and 64, O^T at 128
+  griddep_wait();
+  griddep_launch_dependents();
+
+  const int bh = (int)(blockIdx.x / (unsigned)a.nsplit), split = (int)(blockIdx.x - (unsigned)bh * a.nsplit);
+  const int b = bh / a.Hkv, kvh = bh - b * a.Hkv, q0 = blockIdx.y * N, T = a.T, nq = min(N, a.Q - q0);
+  const int64_t p0l = a.pos0[b];
+  const bool valid = p0l >= 0 && p0l + T <= a.max_ctx;
+  if (!valid && split == 0 && blockIdx.y == 0 && tid == 0) atomicOr(&g_kv4_status, SQ_DEV_BAD_POSITION);
+  const int p0 = valid ? (int)p0l : 0, len = valid ? p0 + T : 0;
+  const int tiles = (len + kT4Keys - 1) / kT4Keys;
+  const int t0 = (int)((int64_t)split * tiles / a.nsplit), t1 = (int)((int64_t)(split + 1) * tiles / a.nsplit);
+  const int n = t1 - t0;
+  const int64_t row = (int64_t)bh * a.max_ctx;  // of the cache
+
+  // ---- the queries, rotated in fp32, by one power of two for all (the largest to
+  // [2^10, 2^11)), as two fp16 terms; warps 0 .. 7 take every eighth
+  float2* cs = reinterpret_cast<float2*>(smem + kT4OffP);  // (the weights come later)
+  if (n > 0) {
+    for (int i = tid; i < min(T, N) * (kHeadDim / 2); i += kT4Threads) {
+      const int k = i / (kHeadDim / 2);
+      const RopeCS r = rope_cs_pair(p0 + (T <= N ? k : (q0 + k) % T), a.rf.f[i % (kHeadDim / 2)]);
+      cs[i] = make_float2(r.c.h, r.s.h);
+    }
+    __syncthreads();
+    float v[N / 8][4];
+    if (warp < 8) {
+#pragma unroll
+      for (int j = 0; j < N / 8; ++j) {
+        const int i = warp + 8 * j, q = q0 + i;
+        v[j][0] = v[j][1] = v[j][2] = v[j][3] = 0.0f;  // d = lane + 32 e
+        if (i < nq) {
+          const int hg = q / T, t = q - hg * T;
+          const __half* x = a.qkv + (((int64_t)b * T + t) * (a.Hq + 2 * a.Hkv) + kvh * a.G + hg) * kHeadDim + lane;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float2 r = cs[(T <= N ? t : i) * (kHeadDim / 2) + lane + 32 * e];
+            const float x1 = __half2float(x[32 * e]), x2 = __half2float(x[32 * e + 64]);
+            v[j][e] = x1 * r.x - x2 * r.y;
+            v[j][e + 2] = x2 * r.x + x1 * r.y;
+          }
+        }
+        float am = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (isfinite(v[j][e])) am = fmaxf(am, fabsf(v[j][e]));
+        am = warp_max(am);
+        if (lane == 0) atomicMax(&s->amax, __float_as_int(am));
+      }
+    }
+    __syncthreads();
+    const int ex = s->amax ? max((s->amax >> 23) - 127, -100) : 10;
+    const float up = __uint_as_float((uint32_t)(127 + 10 - ex) << 23);
+    if (warp < 8) {
+#pragma unroll
+      for (int j = 0; j < N / 8; ++j) {
+        const int i = warp + 8 * j;
+        float sum = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          __half hi, lo;
+          k4_split(v[j][e] * up, hi, lo);
+          sum += __half2float(hi) + __half2float(lo);
+          const int d = lane + 32 * e, k = d & 7, half = d >> 6;
+          const uint32_t at = kT4OffQ + half * kT4QRows + t4_piece(i, d >> 3) + ((k & 3) * 2 + (k >> 2)) * 2;
+          *reinterpret_cast<__half*>(smem + at) = hi;
+          *reinterpret_cast<__half*>(smem + at + 2 * kT4QRows) = lo;
+        }
+        sum = warp_sum(sum);
+        if (lane == 0) {
+          s->qsum[i] = sum;
+          s->lim[i] = p0 + (q0 + i) % T;
+          s->m[i] = -INFINITY;
+          s->neg[i] = INFINITY;
+        }
+      }
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  // scores in units of log 2
+  const float unit = 0.08838834764831845f * 1.4426950408889634f *
+                     __uint_as_float((uint32_t)(127 + (s->amax ? max((s->amax >> 23) - 127, -100) : 10) - 10) << 23);
+  __syncthreads();
+
+  // registers: 512 threads x 128 at launch; the softmax warps take 208, the others
+  // keep 96 (128 x 208 + 384 x 96 <= 512 x 128)
+  if (warp >= 4) {
+   asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+   if (warp == 13) {
+    if (lane == 0) {
+      // ------------------------------------------------------------- copies
+      int t = 0;
+      bool fine = true;
+      for (; t < n; ++t) {
+        const int p = t % kT4Stages;
+        if (t >= kT4Stages &&
+            !(fine = tc_wait(T4_BAR(c_empty) + 8 * p, ((t / kT4Stages) & 1) ^ 1, &s->dead, &g_kv4_status)))
+          break;
+        // (the cache may end inside the tile, after a group of 16)
+        const int64_t key = (int64_t)(t0 + t) * kT4Keys;
+        const uint32_t rows = (uint32_t)min((int64_t)kT4Keys, a.max_ctx - key);
+        uint8_t* to = smem + kT4OffC + p * kT4Stage;
+        mbar_arrive_expect_tx(&s->c_full[p], rows * 136);
+        bulk_g2s(to, a.c.kc + (row + key) * 64, rows * 64, &s->c_full[p]);
+        bulk_g2s(to + kT4Codes, a.c.vc + (row + key) * 64, rows * 64, &s->c_full[p]);
+        bulk_g2s(to + 2 * kT4Codes, a.c.kp + (row + key) * 2, rows * 4, &s->c_full[p]);
+        bulk_g2s(to + 2 * kT4Codes + kT4Keys * 4, a.c.vp + (row + key) * 2, rows * 4, &s->c_full[p]);
+      }
+      if (!fine)  // what was asked for has to arrive
+        for (int i = max(t - kT4Stages, 0); i < t; ++i)
+          mbar_wait_bounded(&s->c_full[i % kT4Stages], (i / kT4Stages) & 1, 1u << 20);
+    }
+   } else if (warp == 12) {
+    if (lane == 0) {
+      // ------------------------------------------------------------- products
+      const uint32_t id_qk = (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((128u >> 4) << 24);
+      const uint32_t id_pv = id_qk | (1u << 16);  // of the weights queries run
+      bool fine = true;
+      for (int t = 0; fine && t <= n; ++t) {
+        if (n == 0) break;
+        if (t < n) {
+          const int p = t & 1;
+          if (!(fine = tc_wait(T4_BAR(k_full) + 8 * p, (t >> 1) & 1, &s->dead, &g_kv4_status))) break;
+          tc_fence_after();
+          const uint64_t kd = sw128_desc(base + p * kT4Tile), qd = sw128_desc(base + kT4OffQ);
+#pragma unroll
+          for (int term = 0; term < 2; ++term)
+#pragma unroll
+            for (int kk = 0; kk < kHeadDim / 16; ++kk)
+              tc_mma_f16(tmem + 64 * p, kd + (kk >> 2) * (kT4Tile / 2 / 16) + (kk & 3) * 2,
+                         qd + term * (2 * kT4QRows / 16) + (kk >> 2) * (kT4QRows / 16) + (kk & 3) * 2, id_qk, term + kk > 0);
+          tc_commit_at(T4_BAR(s_full) + 8 * p);
+        }
+        if (t > 0) {
+          const int p = (t - 1) & 1, ph = ((t - 1) >> 1) & 1;
+          if (!(fine = tc_wait(T4_BAR(v_full) + 8 * p, ph, &s->dead, &g_kv4_status) &&
+                       tc_wait(T4_BAR(p_ready) + 8 * p, ph, &s->dead, &g_kv4_status)))
+            break;
+          tc_fence_after();
+          const uint64_t vd = sw128_desc(base + kT4OffV + p * kT4Tile), pd = t4_desc_mn(base + kT4OffP);
+#pragma unroll
+          for (int kk = 0; kk < kT4Keys / 16; ++kk)
+            tc_mma_f16(tmem + 128, vd + (kk >> 2) * (kT4Tile / 2 / 16) + (kk & 3) * 2, pd + kk * (16 * 128 / 16),
+                       id_pv, t > 1 || kk > 0);
+          tc_commit_at(T4_BAR(pv_done) + 8 * p);
+        }
+      }
+      if (!fine) {  // what was issued still reads shared memory and writes TMEM
+        tc_commit_at(T4_BAR(drain));
+        mbar_wait_bounded(&s->drain, 0u, 1u << 20);
+      }
+    }
+   } else if (warp < 8) {
+    // --------------------------------------------------------------- keys' codes to operands
+    const int ct = tid - 128, t4 = ct & 3;
+    for (int t = 0; t < n; ++t) {
+      const int p = t & 1, ph = (t >> 1) & 1, c_at = t % kT4Stages;
+      const uint8_t* from = smem + kT4OffC + c_at * kT4Stage;
+      tc_wait(T4_BAR(c_full) + 8 * c_at, (t / kT4Stages) & 1, &s->dead, &g_kv4_status);
+      uint4 c[4];  // pieces ct + 128 i: key / 4, 16 bytes of its 64
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c[i] = *reinterpret_cast<const uint4*>(from + (ct + 128 * i) * 16);
+      __syncwarp();
+      if (lane == 0) tc_arrive(T4_BAR(c_empty) + 8 * c_at);
+      if (t >= 2) tc_wait(T4_BAR(s_full) + 8 * p, ph ^ 1, &s->dead, &g_kv4_status);  // (the tile two before is done with)
+      uint8_t* to = smem + p * kT4Tile + (t4 >> 1) * (kT4Tile / 2);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t o[4];
+          int4x8_to_f16x2(w[j], o);
+          *reinterpret_cast<uint4*>(to + t4_piece((ct + 128 * i) >> 2, 4 * t4 + j)) = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) tc_arrive(T4_BAR(k_full) + 8 * p);
+    }
+   } else if (warp < 12) {
+    // --------------------------------------------------------------- values' codes to operands
+    const int u = lane & 7, kg = (warp - 8) * 4 + (lane >> 3);  // dimensions 16 u .. of eight keys
+    for (int t = 0; t < n; ++t) {
+      const int p = t & 1, ph = (t >> 1) & 1, c_at = t % kT4Stages;
+      const uint8_t* from = smem + kT4OffC + c_at * kT4Stage + kT4Codes + kg * 512 + u * 16;
+      tc_wait(T4_BAR(c_full) + 8 * c_at, (t / kT4Stages) & 1, &s->dead, &g_kv4_status);
+      uint4 c[4];  // four pairs of positions
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c[i] = *reinterpret_cast<const uint4*>(from + i * 128);
+      __syncwarp();
+      if (lane == 0) tc_arrive(T4_BAR(c_empty) + 8 * c_at);
+      if (t >= 2) tc_wait(T4_BAR(pv_done) + 8 * p, ph ^ 1, &s->dead, &g_kv4_status);
+      // dimension 16 u + 4 j + e in row (4 j + e) 8 + u: eight lanes, eight bank groups
+      uint8_t* to = smem + kT4OffV + p * kT4Tile + (kg >> 3) * (kT4Tile / 2) + u * 128 + (((kg & 7) ^ u) << 4);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t o[4][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          int4x8_to_f16x2(j == 0 ? c[i].x : j == 1 ? c[i].y : j == 2 ? c[i].z : c[i].w, o[i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          *reinterpret_cast<uint4*>(to + (4 * j + e) * 1024) = make_uint4(o[0][e], o[1][e], o[2][e], o[3][e]);
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) tc_arrive(T4_BAR(v_full) + 8 * p);
+    }
+   }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    // --------------------------------------------------------------- softmax: a key a thread
+    const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+    const int first = p0;  // a position that every query sees
+    unsigned long long l2[N / 2], z2[N / 2];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) l2[i] = z2[i] = 0;
+    float vcap = 0.0f, vup = 1.0f;  // value scales up to vcap; vup brings them to 2^9
+    for (int t = 0; t < n; ++t) {
+      const int p = t & 1, key = (t0 + t) * kT4Keys + tid;  // (below 2^17)
+      const bool edge = (t0 + t + 1) * kT4Keys - 1 > first;
+      const int c_at = t % kT4Stages;
+      tc_wait(T4_BAR(c_full) + 8 * c_at, (t / kT4Stages) & 1, &s->dead, &g_kv4_status);
+      __syncwarp();
+      const __half2* par = reinterpret_cast<const __half2*>(smem + kT4OffC + c_at * kT4Stage + 2 * kT4Codes) + tid;
+      __half2 k2 = par[0], v2 = par[kT4Keys];
+      if (key >= len) k2 = v2 = __float2half2_rn(0.0f);
+      const float2 kf = __half22float2(k2), vf = __half22float2(v2);
+      const float ks = kf.x * unit, k0 = fmaf(8.0f, kf.x, kf.y) * unit;
+      const float w = vf.x, wl = fmaf(8.0f, vf.x, vf.y);
+      tc_wait(T4_BAR(s_full) + 8 * p, (t >> 1) & 1, &s->dead, &g_kv4_status);
+      __syncwarp();
+      tc_fence_after();
+      if (lane == 0) tc_arrive(T4_BAR(c_empty) + 8 * c_at);
+      uint32_t v[N];
+      const uint32_t ts = tmem + 64 * p + lanes, to = tmem + 128 + lanes;
+      // v: scores less the running maxima
+      auto scores = [&](bool less) {
+#pragma unroll
+        for (int i = 0; i < N; i += 16) tm_ld16(ts + i, v + i);
+        tm_wait_ld();
+#pragma unroll
+        for (int i = 0; i < N; i += 16) tm_loaded16(v + i);
+        const unsigned long long kk = f2pack(ks, ks), cc = f2pack(k0, k0);
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+          const ulonglong2 qs = *reinterpret_cast<const ulonglong2*>(&s->qsum[i]);
+          ulonglong2 ng = make_ulonglong2(0, 0);
+          if (less) ng = *reinterpret_cast<const ulonglong2*>(&s->neg[i]);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const unsigned long long off = ffma2_to(cc, e ? qs.y : qs.x, e ? ng.y : ng.x);
+            const float2 y = f2unpack(ffma2_to(
+                kk, f2pack(__uint_as_float(v[i + 2 * e]), __uint_as_float(v[i + 2 * e + 1])), off));
+            v[i + 2 * e] = __float_as_uint(y.x);
+            v[i + 2 * e + 1] = __float_as_uint(y.y);
+          }
+        }
+        if (edge) {
+#pragma unroll
+          for (int i = 0; i < N; ++i)
+            if (key > s->lim[i]) v[i] = 0xff800000u;
+        }
+      };
+      scores(true);
+      float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int i = 0; i < N; i += 8)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          m4[e] = fmaxf(fmaxf(m4[e], __uint_as_float(v[i + e])), __uint_as_float(v[i + e + 4]));
+      const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+      if (t4_any(mx > 5.0f || w > vcap)) {
+        // larger maxima: of the scores themselves, by warps, then all four
+        scores(false);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int x = __float_as_int(fmaxf(__uint_as_float(v[i]), -INFINITY)), o = __reduce_max_sync(0xffffffffu, x ^ ((x >> 31) & 0x7fffffff));
+          if (lane == 0) s->wm[warp][i] = __int_as_float(o ^ ((o >> 31) & 0x7fffffff));
+        }
+        const float vw = warp_max(w);
+        if (lane == 0) s->wv[warp] = vw;
+        named_bar_sync(1, 128);
+        if (tid < N) {
+          const float mo = s->m[tid];
+          const float mn = fmaxf(mo, fmaxf(fmaxf(s->wm[0][tid], s->wm[1][tid]), fmaxf(s->wm[2][tid], s->wm[3][tid])));
+          s->m[tid] = mn;
+          s->neg[tid] = -mn;
+          s->fac[tid] = mo == -INFINITY ? 0.0f : ex2(mo - mn);
+        }
+        const float vm = fmaxf(fmaxf(s->wv[0], s->wv[1]), fmaxf(s->wv[2], s->wv[3]));
+        float fv = 1.0f;
+        if (vm > vcap) {  // the power of two above vm becomes 2^9: weights up to 2^5 stay below 2^15
+          const float cap = __uint_as_float(((__float_as_uint(vm) >> 23) + 1) << 23), up = 512.0f / cap;
+          fv = up / vup;
+          vcap = cap;
+          vup = up;
+        }
+        named_bar_sync(1, 128);
+        if (t > 0) {
+          tc_wait(T4_BAR(pv_done) + 8 * (p ^ 1), ((t - 1) >> 1) & 1, &s->dead, &g_kv4_status);
+          __syncwarp();
+          tc_fence_after();
+#pragma unroll
+          for (int i = 0; i < N; i += 16) {
+            uint32_t o[16];
+            tm_ld16(to + i, o);
+            tm_wait_ld();
+            tm_loaded16(o);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * (s->fac[i + e] * fv));
+            tm_st16(to + i, o);
+          }
+#pragma unroll
+          for (int i = 0; i < N / 2; ++i) {
+            const unsigned long long f = f2pack(s->fac[2 * i], s->fac[2 * i + 1]);
+            asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(l2[i]) : "l"(f));
+            asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(z2[i]) : "l"(f));
+          }
+          tm_wait_st();
+        }
+        scores(true);
+      }
+      // weights: to the sums, and times the value's scale to the products
+      // (the products of the tile before read the place that these go to)
+      if (t > 0) tc_wait(T4_BAR(pv_done) + 8 * (p ^ 1), ((t - 1) >> 1) & 1, &s->dead, &g_kv4_status);
+      __syncwarp();
+      const float ws = w * vup;
+      const unsigned long long wl2 = f2pack(wl, wl);
+      uint8_t* at = smem + kT4OffP + tid * 128;
+      auto weights = [&](auto apart) {
+#pragma unroll
+        for (int i = 0; i < N; i += 8) {
+          uint32_t h[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float a0 = __uint_as_float(v[i + 2 * e]), a1 = __uint_as_float(v[i + 2 * e + 1]);
+            const float x0 = ex2(a0), x1 = ex2(a1);
+            const unsigned long long pr = f2pack(x0, x1);
+            const int j = i / 2 + e;
+            l2[j] = fadd2(l2[j], pr);
+            if constexpr (apart.value) {
+              const bool s0 = a0 != -INFINITY, s1 = a1 != -INFINITY;
+              z2[j] = ffma2_to(pr, f2pack(s0 ? wl : 0.0f, s1 ? wl : 0.0f), z2[j]);
+              h[e] = pack_f16x2(s0 ? x0 * ws : 0.0f, s1 ? x1 * ws : 0.0f);
+            } else {
+              z2[j] = ffma2_to(pr, wl2, z2[j]);
+              h[e] = pack_f16x2(x0 * ws, x1 * ws);
+            }
+          }
+          *reinterpret_cast<uint4*>(at + (((i >> 3) ^ (tid & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+        }
+      };
+      // (a row that one query sees and another does not may hold a NaN)
+      if (edge)
+        weights(std::true_type{});
+      else
+        weights(std::false_type{});
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) tc_arrive(T4_BAR(p_ready) + 8 * p);
+    }
+    // ---- sums over the keys' threads, then rows of results, through shared memory
+    float* part = a.part + (((int64_t)bh * a.nsplit + split) * a.Q + q0) * kK4Rec;
+    const bool join = a.nsplit > 1;
+    if (n > 0) {
+      // (all products are done: the operands' room is free)
+      tc_wait(T4_BAR(pv_done) + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1, &s->dead, &g_kv4_status);
+      __syncwarp();
+      tc_fence_after();
+      float* red = reinterpret_cast<float*>(smem);               // [2 N][129]
+      float* rows = reinterpret_cast<float*>(smem + kT4OffV);    // [N][129]
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) {
+        const float2 x = f2unpack(l2[i]), y = f2unpack(z2[i]);
+        red[(2 * i) * 129 + tid] = x.x;
+        red[(2 * i + 1) * 129 + tid] = x.y;
+        red[(N + 2 * i) * 129 + tid] = y.x;
+        red[(N + 2 * i + 1) * 129 + tid] = y.y;
+      }
+      const float down = 1.0f / vup;
+      const int d = 16 * (tid & 7) + (tid >> 3);  // this TMEM lane's dimension
+#pragma unroll
+      for (int i = 0; i < N; i += 16) {
+        uint32_t o[16];
+        tm_ld16(tmem + 128 + lanes + i, o);
+        tm_wait_ld();
+        tm_loaded16(o);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) rows[(i + e) * 129 + d] = __uint_as_float(o[e]) * down;
+      }
+      tc_fence_before();
+      named_bar_sync(1, 128);
+      if (tid < 2 * N) {
+        float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int j = 0; j < 128; j += 4)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] += red[tid * 129 + j + e];
+        s->total[tid / N][tid % N] = (x[0] + x[1]) + (x[2] + x[3]);
+      }
+      named_bar_sync(1, 128);
+      for (int i = 0; i < nq; ++i) {
+        const float L = s->total[0][i], x = rows[i * 129 + tid] + s->total[1][i];
+        if (join) {
+          part[i * kK4Rec + 4 + tid] = x;
+          if (tid == 0) {
+            // (natural units, as attention_combine_kernel has them, which takes sums above
+            // zero only: where weights are NaN, and so x is, the record has to count)
+            part[i * kK4Rec] = isnan(L) ? 0.0f : s->m[i] * 0.6931471805599453f;
+            part[i * kK4Rec + 1] = isnan(L) ? 1.0f : L;
+          }
+        } else {
+          const int q = q0 + i, hg = q / T, tok = q - hg * T;
+          a.out[(((int64_t)b * T + tok) * a.Hq + kvh * a.G + hg) * kHeadDim + tid] =
+              __float2half_rn(L == 0.0f ? 0.0f : x / L);
+        }
+      }
+    } else {
+      for (int i = 0; i < nq; ++i) {
+        const int q = q0 + i, hg = q / T, tok = q - hg * T;
+        if (!join)
+          a.out[(((int64_t)b * T + tok) * a.Hq + kvh * a.G + hg) * kHeadDim + tid] = __float2half_rn(0.0f);
+        else if (tid < 2)
+          part[i * kK4Rec + tid] = tid ? 0.0f : -INFINITY;
+      }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 12)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256) : "memory");
+}
+#undef T4_BAR
+
+// CTAs a group of queries: such a number of rounds over the SMs that a CTA's tiles
+// and what it costs besides (about six) are over soonest.
+static int64_t t4_shares(int64_t groups, int64_t max_ctx) {
+  const int64_t tiles = (max_ctx + kT4Keys - 1) / kT4Keys, sms = device_sm_count();
+  int64_t best = 1, cost = INT64_MAX;
+  for (int64_t S = 1; S <= tiles && S <= 64; ++S) {
+    const int64_t c = (groups * S + sms - 1) / sms * ((tiles + S - 1) / S + 6) + (S > 1 ? 4 : 0);
+    if (c < cost) {
+      cost = c;
+      best = S;
+    }
+  }
+  return best;
+}
+static int64_t t4_groups(int64_t Q) { return (Q + kT4Max - 1) / kT4Max; }
+
+template <int N>
+static cudaError_t launch_kv4_tc(KV4AttnArgs a, int Z, cudaStream_t st) {
+  static std::mutex mu;
+  static bool ready[64] = {false};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  {
+    std::lock_guard<std::mutex> lock(mu);
+    if (!ready[dev]) {
+      e = cudaFuncSetAttribute(attention_kv4_tc_kernel<N>, cudaFuncAttributeMaxDynamicSharedMemorySize, kT4Smem);
+      if (e != cudaSuccess) return e;
+      ready[dev] = true;
+    }
+  }
+  a.nsplit = (int)t4_shares((int64_t)a.B * a.Hkv * t4_groups(a.Q), a.max_ctx);
+  a.cluster = 0;
+  e = launch_pdl(attention_kv4_tc_kernel<N>, dim3((unsigned)(a.nsplit * a.B * a.Hkv), (unsigned)Z),
+                 dim3(kT4Threads), (size_t)kT4Smem, st, a);
+  if (e != cudaSuccess || a.nsplit == 1) return e;
+  return launch_attention_combine(a.part, a.B, a.T, a.Hq, a.Hkv, a.nsplit, a.out, st);
+}
+
 constexpr int kK4MaxCluster = 16;
 constexpr int kK4PerSm = 3;
 
@@ -722,6 +1312,15 @@ static cudaError_t k4_resident(int S, int* n) {
 }
 
 static int k4_rows(int64_t Q) { return Q <= 8 ? 1 : 2; }
+// Which of the two kernels for more than eight queries: tcgen05 where a code would be
+// converted twice or more (Q > 16) and there is work for its longer chain.  28 / 4
+// heads, five tokens, us here and in attention_kv4_kernel<2>: one sequence of 2000
+// 16.1, 13.7, of 8000 20.5, 21.5, of 30000 28.9, 31.3; 16 of 500 18.9, 17.4, of 2000
+// 26.3, 31.5, of 30000 159, 282.  Up to sixteen queries (40 / 8 heads, three tokens,
+// 16 of 30000: 250, 193) the other one needs its products once.
+static bool k4_long(int64_t heads, int64_t Q, int64_t max_ctx) {
+  return Q > 16 && heads * ((Q + 15) / 16) * max_ctx >= 100000;
+}
 
 // CTAs that share the keys of a group of queries: as many as fill the SMs, at
 // least a step of 32 keys for each of a CTA's warps.
@@ -734,7 +1333,10 @@ static int64_t k4_shares(int64_t groups, int64_t max_ctx) {
 
 size_t attention_kv4_workspace_bytes(int B, int T, int Hq, int Hkv, int64_t max_ctx) {
   const int64_t Q = (int64_t)(Hq / Hkv) * T, kq = 8 * k4_rows(Q), groups = (int64_t)B * Hkv * ((Q + kq - 1) / kq);
-  const int64_t S = groups ? k4_shares(groups, max_ctx) : 1;
+  const int64_t heads = (int64_t)B * Hkv;
+  const int64_t S = !groups                       ? 1
+                    : k4_long(heads, Q, max_ctx) ? t4_shares(heads * t4_groups(Q), max_ctx)
+                                                 : k4_shares(groups, max_ctx);
   return (S > 1 ? (size_t)(B * (int64_t)Hkv * S * Q) * kK4Rec * sizeof(float) : 0) + 16;
 }
 
@@ -803,6 +1405,10 @@ cudaError_t launch_attention_kv4(const __half* qkv, int B, int T, int Hq, int Hk
   a.Q = a.G * T;
   a.max_ctx = max_ctx;
   a.rf = rope_freq(theta);
+  if (k4_long((int64_t)B * Hkv, a.Q, max_ctx)) {
+    const int Z = (int)t4_groups(a.Q), n = (a.Q + Z - 1) / Z;
+    return n <= 32 ? launch_kv4_tc<32>(a, (a.Q + 31) / 32, st) : launch_kv4_tc<48>(a, Z, st);
+  }
   return k4_rows(a.Q) == 1 ? launch_kv4_inst<1>(a, st) : launch_kv4_inst<2>(a, st);
 }
 

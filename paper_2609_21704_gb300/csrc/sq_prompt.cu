@@ -402,61 +402,6 @@ __device__ __forceinline__ uint64_t sw128_desc_mn(uint32_t saddr) {
   return d;
 }
 
-// 32 consecutive columns of this thread's TMEM lane.
-__device__ __forceinline__ void tm_ld32(uint32_t addr, uint32_t* r) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
-      "%15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-      : "r"(addr));
-}
-__device__ __forceinline__ void tm_st32(uint32_t addr, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, "
-      "%14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(r[0]),
-      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
-      "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
-      "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr)
-      : "memory");
-}
-// Waits for this thread's TMEM loads.  tm_loaded32: 32 registers that were
-// loaded before the last wait (so that nothing that reads them moves above it).
-__device__ __forceinline__ void tm_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tm_loaded32(uint32_t* r) {
-#pragma unroll
-  for (int i = 0; i < 32; i += 8)
-    asm volatile(""
-                 : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]),
-                   "+r"(r[i + 6]), "+r"(r[i + 7]));
-}
-__device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-__device__ __forceinline__ unsigned long long ffma2_to(unsigned long long a, unsigned long long b,
-                                                       unsigned long long c) {
-  unsigned long long d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ unsigned long long fadd2(unsigned long long a, unsigned long long b) {
-  unsigned long long d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-
 struct PromptArgs {
   const PromptWork* work;
   const __half* vc;
@@ -487,51 +432,12 @@ struct PromptBars {
 static_assert(sizeof(PromptBars) <= 512, "barriers fit their place");
 
 // Waits at most two seconds, and not at all once another wait has run out.
-__device__ __forceinline__ uint64_t pr_clock_ns() {
-  uint64_t t;
-  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-  return t;
-}
-// (barriers by their shared address: the roles' registers are few)
-__device__ __forceinline__ bool pr_try(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n"
-      ".reg .pred p;\n"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
-      "selp.u32 %0, 1, 0, p;\n"
-      "}\n"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
 __device__ __forceinline__ bool pr_wait(uint32_t bar, uint32_t parity, PromptBars* s) {
-  volatile int* dead = &s->dead;
-  uint64_t start = 0;
-  for (uint32_t i = 1;; ++i) {
-    if (pr_try(bar, parity)) return true;
-    if ((i & 63) == 0) {
-      if (*dead) return false;
-      const uint64_t now = pr_clock_ns();
-      if (start == 0) start = now;
-      if (now - start > 2000000000ull) break;
-    }
-  }
-  *dead = 1;
-  atomicOr(&g_prompt_status, SQ_DEV_TIMEOUT);
-  return false;
-}
-__device__ __forceinline__ void pr_arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+  return tc_wait(bar, parity, &s->dead, &g_prompt_status);
 }
 __device__ __forceinline__ void pr_expect(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void pr_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-
 // The blocks of an item that half h of its rows sees any key of.
 __device__ __forceinline__ int pr_blocks(const PromptItem& it, int G, int h) {
   const int rows = it.len * G;
@@ -678,7 +584,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
           const uint64_t o = (uint64_t)((kk >> 2) * (kPrTile / 2 / 16) + (kk & 3) * 2);
           tc_mma_f16(tmem + h * 128, qd + o, kd + o, id_qk, kk > 0);
         }
-        pr_commit(PR_BAR(s_full) + 8 * (h));
+        tc_commit_at(PR_BAR(s_full) + 8 * (h));
       };
       for (int r = 0, w; fine && (w = pick(r)) < total; ++r) {
         const PromptItem it = items[w / a.Hkv];
@@ -690,9 +596,9 @@ __global__ void __launch_bounds__(kPrThreads, 1)
 #pragma unroll
         for (int h = 0; h < 2; ++h)
           if (nb[h] > 0) qk(h, nk % kPrK);
-        pr_commit(PR_BAR(k_empty) + 8 * (nk % kPrK));
+        tc_commit_at(PR_BAR(k_empty) + 8 * (nk % kPrK));
         ++nk;
-        if (nm == 1) pr_commit(PR_BAR(q_empty));
+        if (nm == 1) tc_commit_at(PR_BAR(q_empty));
         for (int j = 0; fine && j < nm; ++j) {
           if (j + 1 < nm && !(fine = keys())) break;
           if (!(fine = pr_wait(PR_BAR(v_ready) + 8 * (nv % kPrV), (nv / kPrV) & 1u, s))) break;
@@ -712,21 +618,21 @@ __global__ void __launch_bounds__(kPrThreads, 1)
             }
             if (!fine) break;
             ++np[h];
-            pr_commit(PR_BAR(o_done) + 8 * (h));
+            tc_commit_at(PR_BAR(o_done) + 8 * (h));
             if (j + 1 < nb[h]) qk(h, nk % kPrK);
           }
           if (!fine) break;
-          pr_commit(PR_BAR(v_empty) + 8 * (nv % kPrV));
+          tc_commit_at(PR_BAR(v_empty) + 8 * (nv % kPrV));
           ++nv;
           if (j + 1 < nm) {
-            pr_commit(PR_BAR(k_empty) + 8 * (nk % kPrK));
+            tc_commit_at(PR_BAR(k_empty) + 8 * (nk % kPrK));
             ++nk;
           }
-          if (j + 2 == nm) pr_commit(PR_BAR(q_empty));
+          if (j + 2 == nm) tc_commit_at(PR_BAR(q_empty));
         }
       }
       if (!fine) {  // what was issued still writes TMEM
-        pr_commit(PR_BAR(drain));
+        tc_commit_at(PR_BAR(drain));
         mbar_wait_bounded(&s->drain, 0u, 1u << 20);
       }
     }
@@ -782,7 +688,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
         }
-        if (lane == 0) pr_arrive(PR_BAR(v_ready) + 8 * (st));
+        if (lane == 0) tc_arrive(PR_BAR(v_ready) + 8 * (st));
       }
     }
    }
@@ -881,7 +787,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
           tm_wait_st();
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) pr_arrive(PR_BAR(p_ready) + 16 * (h) + 8 * (i));  // (32 arrivals of a warp take turns)
+          if (lane == 0) tc_arrive(PR_BAR(p_ready) + 16 * (h) + 8 * (i));  // (32 arrivals of a warp take turns)
         }
         l2 = fadd2(sum[0], sum[1]);
       }
