@@ -700,14 +700,19 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
 // where the four warps agree.  One thread issues the products.
 // attention_kv4_kernel converts a code for every sixteen queries and is bound by
 // mma.sync, 16 cycles an m16n8k16 on each quarter of an SM: 16 x 5 tokens behind
-// 30000, 28 / 4 heads, 282 us.  Here 167, 1.3 us a tile: with neither copies,
-// conversion nor softmax it takes 140, with a third of the products besides 105: the
-// rest are hand-overs (weights written, products, their place free).  Two places for
-// the weights and two tiles of copies in flight instead of one and three: 182; one
-// group for keys and values 196; codes loaded into registers 302.
+// 30000, 28 / 4 heads, 282 us.  Here 155, 1.2 us a tile.  What that is made of (taken
+// with three rounds of CTAs, 163 us in all): without copies, conversion and softmax
+// 140, with a third of the products besides 105; the rest are hand-overs (weights
+// written, products, their place free).  Two places for the weights and two tiles of
+// copies in flight instead of one and three: 182; one group for keys and values 196;
+// codes loaded into registers 302.
 constexpr int kT4Keys = 128, kT4Threads = 512;
 constexpr int kT4Tile = kT4Keys * kHeadDim * 2;  // fp16 operands of a tile's keys (or values)
 constexpr int kT4Max = 48;                       // queries of a CTA
+// The tensor core cuts what it adds to a sum where an fp32 addition rounds: 117 tiles in
+// one sum had a bias of 2.4e-4 of the result (34 tiles 0.7e-4).  So tiles go to six sums
+// in turn, which are added at the end, and no CTA takes more than 24 tiles to each.
+constexpr int kT4Sums = 6, kT4MaxTiles = 24 * kT4Sums;
 constexpr int kT4OffV = 2 * kT4Tile, kT4OffP = 4 * kT4Tile;
 constexpr int kT4P = kT4Keys * 128;              // weights of a tile: 64 queries' places a key
 constexpr int kT4OffQ = kT4OffP + kT4P;      // two terms x two halves of the dimensions
@@ -783,14 +788,14 @@ __global__ void __launch_bounds__(kT4Threads, 1) attention_kv4_tc_kernel(const K
   }
   if (warp == 12) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s->tmem)),
-                 "r"(256)
+                 "r"(512)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *(volatile uint32_t*)&s->tmem;  // S^T at 0 and 64, O^T at 128
+  const uint32_t tmem = *(volatile uint32_t*)&s->tmem;  // S^T at 0 and 64, O^T's places from 128 on, 64 columns each
   griddep_wait();
   griddep_launch_dependents();
 
@@ -920,7 +925,8 @@ __global__ void __launch_bounds__(kT4Threads, 1) attention_kv4_tc_kernel(const K
 #pragma unroll
             for (int kk = 0; kk < kHeadDim / 16; ++kk)
               tc_mma_f16(tmem + 64 * p, kd + (kk >> 2) * (kT4Tile / 2 / 16) + (kk & 3) * 2,
-                         qd + term * (2 * kT4QRows / 16) + (kk >> 2) * (kT4QRows / 16) + (kk & 3) * 2, id_qk, term + kk > 0);
+                         qd + term * (2 * kT4QRows / 16) + (kk >> 2) * (kT4QRows / 16) + (kk & 3) * 2, id_qk,
+                         term + kk > 0);
           tc_commit_at(T4_BAR(s_full) + 8 * p);
         }
         if (t > 0) {
@@ -932,8 +938,8 @@ __global__ void __launch_bounds__(kT4Threads, 1) attention_kv4_tc_kernel(const K
           const uint64_t vd = sw128_desc(base + kT4OffV + p * kT4Tile), pd = t4_desc_mn(base + kT4OffP);
 #pragma unroll
           for (int kk = 0; kk < kT4Keys / 16; ++kk)
-            tc_mma_f16(tmem + 128, vd + (kk >> 2) * (kT4Tile / 2 / 16) + (kk & 3) * 2, pd + kk * (16 * 128 / 16),
-                       id_pv, t > 1 || kk > 0);
+            tc_mma_f16(tmem + 128 + 64 * ((t - 1) % kT4Sums), vd + (kk >> 2) * (kT4Tile / 2 / 16) + (kk & 3) * 2,
+                       pd + kk * (16 * 128 / 16), id_pv, t > kT4Sums || kk > 0);
           tc_commit_at(T4_BAR(pv_done) + 8 * p);
         }
       }
@@ -954,7 +960,8 @@ __global__ void __launch_bounds__(kT4Threads, 1) attention_kv4_tc_kernel(const K
       for (int i = 0; i < 4; ++i) c[i] = *reinterpret_cast<const uint4*>(from + (ct + 128 * i) * 16);
       __syncwarp();
       if (lane == 0) tc_arrive(T4_BAR(c_empty) + 8 * c_at);
-      if (t >= 2) tc_wait(T4_BAR(s_full) + 8 * p, ph ^ 1, &s->dead, &g_kv4_status);  // (the tile two before is done with)
+      // (the tile two before is done with)
+      if (t >= 2) tc_wait(T4_BAR(s_full) + 8 * p, ph ^ 1, &s->dead, &g_kv4_status);
       uint8_t* to = smem + p * kT4Tile + (t4 >> 1) * (kT4Tile / 2);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -963,7 +970,8 @@ __global__ void __launch_bounds__(kT4Threads, 1) attention_kv4_tc_kernel(const K
         for (int j = 0; j < 4; ++j) {
           uint32_t o[4];
           int4x8_to_f16x2(w[j], o);
-          *reinterpret_cast<uint4*>(to + t4_piece((ct + 128 * i) >> 2, 4 * t4 + j)) = make_uint4(o[0], o[1], o[2], o[3]);
+          *reinterpret_cast<uint4*>(to + t4_piece((ct + 128 * i) >> 2, 4 * t4 + j)) =
+              make_uint4(o[0], o[1], o[2], o[3]);
         }
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -1068,7 +1076,8 @@ __global__ void __launch_bounds__(kT4Threads, 1) attention_kv4_tc_kernel(const K
         scores(false);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          const int x = __float_as_int(fmaxf(__uint_as_float(v[i]), -INFINITY)), o = __reduce_max_sync(0xffffffffu, x ^ ((x >> 31) & 0x7fffffff));
+          const int x = __float_as_int(fmaxf(__uint_as_float(v[i]), -INFINITY));  // (a NaN is none)
+          const int o = __reduce_max_sync(0xffffffffu, x ^ ((x >> 31) & 0x7fffffff));
           if (lane == 0) s->wm[warp][i] = __int_as_float(o ^ ((o >> 31) & 0x7fffffff));
         }
         const float vw = warp_max(w);
@@ -1094,16 +1103,18 @@ __global__ void __launch_bounds__(kT4Threads, 1) attention_kv4_tc_kernel(const K
           tc_wait(T4_BAR(pv_done) + 8 * (p ^ 1), ((t - 1) >> 1) & 1, &s->dead, &g_kv4_status);
           __syncwarp();
           tc_fence_after();
+#pragma unroll 1
+          for (int k = 0; k < min(t, kT4Sums); ++k)
 #pragma unroll
-          for (int i = 0; i < N; i += 16) {
-            uint32_t o[16];
-            tm_ld16(to + i, o);
-            tm_wait_ld();
-            tm_loaded16(o);
+            for (int i = 0; i < N; i += 16) {
+              uint32_t o[16];
+              tm_ld16(to + 64 * k + i, o);
+              tm_wait_ld();
+              tm_loaded16(o);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * (s->fac[i + e] * fv));
-            tm_st16(to + i, o);
-          }
+              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * (s->fac[i + e] * fv));
+              tm_st16(to + 64 * k + i, o);
+            }
 #pragma unroll
           for (int i = 0; i < N / 2; ++i) {
             const unsigned long long f = f2pack(s->fac[2 * i], s->fac[2 * i + 1]);
@@ -1176,12 +1187,20 @@ __global__ void __launch_bounds__(kT4Threads, 1) attention_kv4_tc_kernel(const K
       const int d = 16 * (tid & 7) + (tid >> 3);  // this TMEM lane's dimension
 #pragma unroll
       for (int i = 0; i < N; i += 16) {
-        uint32_t o[16];
-        tm_ld16(tmem + 128 + lanes + i, o);
-        tm_wait_ld();
-        tm_loaded16(o);
+        float x[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) rows[(i + e) * 129 + d] = __uint_as_float(o[e]) * down;
+        for (int e = 0; e < 16; ++e) x[e] = 0.0f;
+#pragma unroll 1
+        for (int k = 0; k < min(n, kT4Sums); ++k) {
+          uint32_t o[16];
+          tm_ld16(tmem + 128 + 64 * k + lanes + i, o);
+          tm_wait_ld();
+          tm_loaded16(o);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[e] += __uint_as_float(o[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) rows[(i + e) * 129 + d] = x[e] * down;
       }
       tc_fence_before();
       named_bar_sync(1, 128);
@@ -1224,17 +1243,18 @@ __global__ void __launch_bounds__(kT4Threads, 1) attention_kv4_tc_kernel(const K
   __syncthreads();
   tc_fence_after();
   if (warp == 12)
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 #undef T4_BAR
 
 // CTAs a group of queries: such a number of rounds over the SMs that a CTA's tiles
-// and what it costs besides (about six) are over soonest.
+// and what it costs besides (about twelve) are over soonest (16 x 5 tokens behind
+// 30000, 28 / 4 heads: two CTAs a head in one round 154 us, seven in three 168).
 static int64_t t4_shares(int64_t groups, int64_t max_ctx) {
   const int64_t tiles = (max_ctx + kT4Keys - 1) / kT4Keys, sms = device_sm_count();
   int64_t best = 1, cost = INT64_MAX;
-  for (int64_t S = 1; S <= tiles && S <= 64; ++S) {
-    const int64_t c = (groups * S + sms - 1) / sms * ((tiles + S - 1) / S + 6) + (S > 1 ? 4 : 0);
+  for (int64_t S = (tiles + kT4MaxTiles - 1) / kT4MaxTiles; S <= tiles && S <= 64; ++S) {
+    const int64_t c = (groups * S + sms - 1) / sms * ((tiles + S - 1) / S + 12) + (S > 1 ? 4 : 0);
     if (c < cost) {
       cost = c;
       best = S;
@@ -1316,7 +1336,7 @@ static int k4_rows(int64_t Q) { return Q <= 8 ? 1 : 2; }
 // converted twice or more (Q > 16) and there is work for its longer chain.  28 / 4
 // heads, five tokens, us here and in attention_kv4_kernel<2>: one sequence of 2000
 // 16.1, 13.7, of 8000 20.5, 21.5, of 30000 28.9, 31.3; 16 of 500 18.9, 17.4, of 2000
-// 26.3, 31.5, of 30000 159, 282.  Up to sixteen queries (40 / 8 heads, three tokens,
+// 26.3, 31.5, of 30000 155, 282.  Up to sixteen queries (40 / 8 heads, three tokens,
 // 16 of 30000: 250, 193) the other one needs its products once.
 static bool k4_long(int64_t heads, int64_t Q, int64_t max_ctx) {
   return Q > 16 && heads * ((Q + 15) / 16) * max_ctx >= 100000;

@@ -90,6 +90,32 @@ def test_growing_maxima_rescale(grow):
     _check(out, qkv, vals, cache, B, T, Hq, Hkv, [L - T], 1.0 if grow == "values" else 4.0)
 
 
+@pytest.mark.parametrize("B,C", [(8, 13312), (1, 131072)])
+def test_sums_over_many_tiles_keep_their_precision(B, C):
+    """About a hundred tiles a CTA, and the longest cache: as a whole within the root
+    of the sum of the output's rounding and a weight's (2^-11 / sqrt(3) at most of a
+    uniform mantissa, 2.8e-4 each at the worst, 2.0e-4 on average), and a fifth for
+    what the sums lose."""
+    T, Hq, Hkv = 5, 56, 8
+    if B == 1:
+        Hq, Hkv = 7, 1
+    rng = np.random.default_rng(B)
+    pos0 = [C - T] * B
+    cache, vals = _random_cache(rng, 1, Hkv, C, pos0[:1], T)
+    qkv = rng.normal(0, 1, (T, (Hq + 2 * Hkv) * D)).astype(np.float16)
+    dc = [_t(c).repeat(B, 1, 1, 1) for c in cache]
+    out = torch.empty(B * T, Hq * D, dtype=torch.float16, device=dev())
+    _attention(np.tile(qkv, (B, 1)), B, T, Hq, Hkv, pos0, dc, out)
+    assert sq.sq_check() == 0
+    pos = C - T + np.arange(T)
+    q = oracle.rope(qkv[:, :Hq * D].astype(np.float64), pos, Hq, D, THETA).reshape(T, Hq, D)
+    ref = oracle.attention(q, vals[0][0].transpose(1, 0, 2), vals[1][0].transpose(1, 0, 2), pos).reshape(T, -1)
+    got = out.float().cpu().numpy().astype(np.float64).reshape(B, T, -1)
+    assert (got == got[:1]).all()
+    rel = np.linalg.norm(got[0] - ref) / np.linalg.norm(ref)
+    assert rel <= 2.8e-4 * 1.2, rel
+
+
 def test_heads_of_very_different_size():
     """One power of two serves the queries of a CTA: those of a head a ten
     thousandth as large keep their bits."""
