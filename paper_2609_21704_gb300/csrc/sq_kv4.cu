@@ -709,9 +709,11 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
 constexpr int kT4Keys = 128, kT4Threads = 512;
 constexpr int kT4Tile = kT4Keys * kHeadDim * 2;  // fp16 operands of a tile's keys (or values)
 constexpr int kT4Max = 48;                       // queries of a CTA
-// The tensor core cuts what it adds to a sum where an fp32 addition rounds: 117 tiles in
-// one sum had a bias of 2.4e-4 of the result (34 tiles 0.7e-4).  So tiles go to six sums
-// in turn, which are added at the end, and no CTA takes more than 24 tiles to each.
+// What the tensor core adds to a sum it cuts where an fp32 addition rounds, and the
+// codes' part of the values does not cancel as the values do (their lowest ones come
+// beside it): 117 tiles in one sum were off by 2.4e-4 of the result, 34 by 0.7e-4.  So
+// tiles go to six sums in turn, which are added at the end, and no CTA takes more than
+// 24 tiles to each.
 constexpr int kT4Sums = 6, kT4MaxTiles = 24 * kT4Sums;
 constexpr int kT4OffV = 2 * kT4Tile, kT4OffP = 4 * kT4Tile;
 constexpr int kT4P = kT4Keys * 128;              // weights of a tile: 64 queries' places a key
