@@ -268,10 +268,13 @@ __global__ void __launch_bounds__(kLpThreads, kLpPerSm) logprobs_kernel(const Lo
     sum.S = warp_sum((s0.x + s0.y) + (s1.x + s1.y));
     sum.E = warp_sum((e0.x + e0.y) + (e1.x + e1.y));
     sum.eq = __reduce_add_sync(0xffffffffu, eq);
-    // y is `skew` less than (z - m) c
-    const float skew = fmaf(-m, c, -b), f = lp_ex2(skew);
-    sum.E = f * fmaf(skew, sum.S, sum.E);
-    sum.S *= f;
+    // y is `skew` less than (z - m) c.  At a small temperature it is large (m c may
+    // be 10^35, rounded), and no entry but the largest has any weight: nothing to put right.
+    if (sum.S > 0.0f) {
+      const float skew = fmaf(-m, c, -b), f = lp_ex2(skew);
+      sum.E = f * fmaf(skew, sum.S, sum.E);
+      sum.S *= f;
+    }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     if (!isnan(sum.E)) break;  // (the whole warp)
   }

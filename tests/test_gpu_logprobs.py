@@ -179,3 +179,23 @@ def test_rows_beyond_32_bit_offsets():
     assert sq.sq_check() == 0
     assert tt[-1].tolist() == [400001, 123, 0] and tt[0].tolist() == [0, 1, 2]
     assert abs(float(ent[0]) - np.log(V)) < 1e-4
+
+
+@pytest.mark.parametrize("T", [1e-4, 1e-6, 1e-9, 1e-30])
+@pytest.mark.parametrize("R,V", [(8, 151936), (8, 90), (800, 4099)])
+def test_small_temperatures(R, V, T):
+    """Down to the smallest temperature only the largest entries have any weight:
+    log probability 0 of one, -log n of n equal ones, far ones down to -1e35."""
+    T = float(np.float32(T))
+    rng = np.random.default_rng(V)
+    z = rng.normal(0, 2, (R, V)).astype(np.float16)
+    z[1] += np.float16(20)
+    z[2, [3, V // 2, V - 1]] = 17.25                     # three equal ones
+    z[3] = -np.abs(z[3]) - np.float16(30)                # all below zero
+    z[4, V - 3] = 65504.0
+    z[5] = -65504.0
+    z[6, ::2] = -np.inf                                  # banned entries
+    z[7] = 12.3
+    best = z.argmax(-1)
+    tokens = np.where(np.arange(R) % 3 == 2, rng.integers(0, V // 2, R) * 2 + 1, best)
+    _check(z, T, tokens, 5)
