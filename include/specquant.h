@@ -430,9 +430,11 @@ SQ_API sq_status sq_spec_drafts(const int32_t* samples, const int32_t* last2, in
  *   p_j = exp(q . k_j / sqrt(D))
  * over the cache, query head h against key/value head h / (Hq / Hkv), out
  * fp16 [N, Hq * D].  Rotated keys are rounded to fp16 once, correctly,
- * rotated queries from fp32; products are exact; sums and the softmax's statistics are fp32;
- * a probability relative to its row's maximum is rounded to fp16 for its
- * product with the value (its sum is not).  What lies in the caches behind a
+ * rotated queries once, from fp32; products are exact; sums and the softmax's
+ * statistics are fp32, of values and probabilities on the tensor core, which cuts
+ * off where an fp32 addition rounds (over any length 2^-14 of the result at
+ * most, where nothing cancels); a probability relative to its row's maximum is
+ * rounded to fp16 for its product with the value (its sum is not).  What lies in the caches behind a
  * token's position, infinities and NaN included, has no effect on its row;
  * scores of -inf have no weight, and a row without any other is zero.  A sequence
  * that does not fit its cache (pos0[b] < 0 or pos0[b] + length > max_ctx)

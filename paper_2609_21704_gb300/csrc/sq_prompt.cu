@@ -27,6 +27,13 @@ constexpr int kPrTile = kPrKeys * kHeadDim * 2;  // bytes of a block's keys (or 
 constexpr int kPrK = 2, kPrV = 3;  // tiles of keys and of values in shared memory
 constexpr int kPrPrepThreads = 256;
 constexpr int kPrMaxBlocks = (int)(kPromptMaxCtx / kPrKeys);
+// Blocks that go to one sum in TMEM.  The tensor core cuts off what it adds to a sum
+// where an fp32 addition rounds, 2^-23 of it at most for each product of sixteen keys:
+// 64 blocks lose 5e-5 of the result where the values have a mean (limit 2^-14), 1024
+// blocks in one sum 8.3e-4, more than the output's rounding to fp16.  So every 64 blocks
+// a row's sums are put aside, and added to what lies there, in fp32 (1300 tokens at the
+// end of 131072, 64 / 1 heads: 5.05 ms, 5.02 in one sum).
+constexpr int kPrSum = 64;
 
 // One piece of work: kPrRows query rows of a sequence (a row is a (token, head
 // of the group) pair, q = t G + g, so a tile is full whatever G is and spans
@@ -44,13 +51,14 @@ struct PromptWork {
   unsigned int* done;  // [groups, Hkv, 2] pieces that have arrived
   uint8_t* odd;        // [Hkv, N] a value of this row is not finite
   float* rec;          // partial results: [record, Hkv, 2][kPrRec]
+  float* aside;        // sums put aside: [CTA, 2][kPrRec]
 };
 // m, l and the weighted values of 128 rows, a row's next value 128 floats on
 constexpr int kPrRec = (kHeadDim + 2) * 128;
 
 struct PromptLayout {
   int64_t max_items, max_recs;
-  size_t item, done, odd, q, rec, bytes;
+  size_t item, done, odd, q, rec, aside, bytes;
 };
 
 // Pieces that a launch may split its work into: twice the SMs.
@@ -69,7 +77,8 @@ static PromptLayout prompt_layout(int B, int64_t N, int Hq, int Hkv, int64_t max
   l.odd = l.done + up((size_t)l.max_recs * 2 * sizeof(unsigned int));
   l.q = l.odd + up((size_t)Hkv * N);
   l.rec = l.q + up((size_t)N * Hq * kHeadDim * sizeof(__half));
-  l.bytes = l.rec + (size_t)l.max_recs * 2 * kPrRec * sizeof(float);
+  l.aside = l.rec + up((size_t)l.max_recs * 2 * kPrRec * sizeof(float));
+  l.bytes = l.aside + (blocks > kPrSum ? (size_t)device_sm_count() * 2 * kPrRec * sizeof(float) : 0);
   return l;
 }
 
@@ -457,7 +466,7 @@ __device__ __forceinline__ int pr_blocks(const PromptItem& it, int G, int h) {
 // other is in its softmax.  TMEM: S0, S1, O0, O1, 128 columns each.
 // The running maximum of a row is let lag by up to 2^kPrSlack before O and the
 // sum are rescaled (the result is the same but for fp16's range), so that O
-// leaves TMEM once, at the end.
+// leaves TMEM once, at the end, and every kPrSum blocks before it.
 // Bound: the chain of a half's block (scores, softmax, weights, products), as its
 // scores have one place.  8000 tokens, 40 / 8 heads: 485 us, 1.35 PFLOP/s, the
 // tensor pipe busy for 59 % of them; 1.83 us for both halves' block, 1.06 of them
@@ -614,7 +623,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
 #pragma unroll
               for (int kk = 4 * half; kk < 4 * half + 4; ++kk)
                 tc_mma_f16_ts(tmem + 256 + h * 128, tmem + h * 128 + kk * 8, vd + kk * (16 * 128 / 16), id_pv,
-                              j > 0 || kk > 0);
+                              j % kPrSum > 0 || kk > 0);
             }
             if (!fine) break;
             ++np[h];
@@ -716,6 +725,32 @@ __global__ void __launch_bounds__(kPrThreads, 1)
         if (j > 0) pr_wait(PR_BAR(o_done) + 8 * (h), (ns & 1u) ^ 1u, s);
         __syncwarp();
         tc_fence_after();
+        if (j % kPrSum == 0 && j > 0) {  // (this block's products begin a sum, once its weights are there)
+          float* aside = a.work->aside + ((int64_t)blockIdx.x * 2 + h) * kPrRec + row;
+          const float2 lp = f2unpack(l2);
+          float f = 0.0f, la = lp.x + lp.y;
+          l2 = 0;
+          if (j > kPrSum) {
+            const float ma = __ldcg(aside + kHeadDim * 128);
+            if (ma != -INFINITY) f = ex2((ma - m) * c);
+            la = fmaf(__ldcg(aside + (kHeadDim + 1) * 128), f, la);
+          }
+          __stcg(aside + kHeadDim * 128, m);
+          __stcg(aside + (kHeadDim + 1) * 128, la);
+#pragma unroll 1
+          for (int i = 0; i < 4; ++i) {
+            uint32_t o[32];
+            tm_ld32(to + 32 * i, o);
+            tm_wait_ld();
+            tm_loaded32(o);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              float x = __uint_as_float(o[e]);
+              if (j > kPrSum) x = fmaf(f, __ldcg(aside + (32 * i + e) * 128), x);
+              __stcg(aside + (32 * i + e) * 128, x);
+            }
+          }
+        }
         // scores in two loads, the second under the first one's maximum
         uint32_t v[128];
         const int key0 = (it.blk0 + j) * kPrKeys;
@@ -754,7 +789,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
           const float mn = fmaxf(m, mb);
           const float f = m == -INFINITY ? 0.0f : ex2((m - mn) * c);
           m = mn;
-          if (j > 0) {
+          if (j % kPrSum > 0) {
             const unsigned long long f2 = f2pack(f, f);
             asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(l2) : "l"(f2));
 #pragma unroll 1
@@ -796,7 +831,13 @@ __global__ void __launch_bounds__(kPrThreads, 1)
       __syncwarp();
       tc_fence_after();
       const float2 lp = f2unpack(l2);
-      const float l = lp.x + lp.y;
+      float l = lp.x + lp.y, fa = 0.0f;
+      const float* aside = a.work->aside + ((int64_t)blockIdx.x * 2 + h) * kPrRec + row;
+      if (nb > kPrSum) {
+        const float ma = __ldcg(aside + kHeadDim * 128);
+        if (ma != -INFINITY) fa = ex2((ma - m) * c);
+        l = fmaf(__ldcg(aside + (kHeadDim + 1) * 128), fa, l);
+      }
       const bool split = it.nsplit > 1;
       const float f = split ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
       const bool odd = *(volatile int*)&s->odd[r & 7] == r + 1;
@@ -809,6 +850,11 @@ __global__ void __launch_bounds__(kPrThreads, 1)
           tm_ld32(to + 32 * i, o);
           tm_wait_ld();
           tm_loaded32(o);
+        }
+        if (nb > kPrSum) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            o[e] = __float_as_uint(fmaf(fa, __ldcg(aside + (32 * i + e) * 128), __uint_as_float(o[e])));
         }
 #pragma unroll
         for (int e = 0; e < 32; ++e) o[e] = nb > 0 ? __float_as_uint(__uint_as_float(o[e]) * f) : 0u;
@@ -951,6 +997,7 @@ cudaError_t launch_prompt(const __half* qkv, const Packed& pk, int Hq, int Hkv, 
   a.init.done = reinterpret_cast<unsigned int*>(w + l.done);
   a.init.odd = w + l.odd;
   a.init.rec = reinterpret_cast<float*>(w + l.rec);
+  a.init.aside = reinterpret_cast<float*>(w + l.aside);
   const int rows = pk.N <= kPrFewRows ? 1 : 2;
   e = launch_pdl(rows == 1 ? prompt_prepare_kernel<1> : prompt_prepare_kernel<2>,
                  dim3((unsigned)((pk.N + rows - 1) / rows + 1)), dim3(kPrPrepThreads), 0, st, qkv, Hq,

@@ -7,7 +7,7 @@ import torch
 
 import paper_2609_21704_gb300 as sq
 from gpu_util import dev
-from serve_ref import D, THETA, prompt
+from serve_ref import D, THETA, attend, prompt, rotated
 
 pytestmark = pytest.mark.gpu
 
@@ -315,3 +315,49 @@ def test_many_sequences(B, n, G, Hkv):
     assert np.array_equal(k.view(np.uint16), rk.view(np.uint16))
     assert np.array_equal(v.view(np.uint16), rv.view(np.uint16))
     _assert(got, ref, bound)
+
+
+def _some_rows(args, lens, pos0, Hq, Hkv, rows):
+    """The reference of `prompt` for some rows of a large batch: (out, bound, kc, vc)."""
+    qkv, off, _, kc, vc = args
+    kc, vc = kc.copy(), vc.copy()
+    out, bound = np.empty((len(rows), Hq * D)), np.empty((len(rows), Hq * D))
+    for b, n in enumerate(lens):
+        new = qkv[off[b]:off[b] + n].astype(np.float64)
+        pos = pos0[b] + np.arange(n)
+        kc[b, :, pos] = rotated(new[:, Hq * D:(Hq + Hkv) * D], pos, Hkv).astype(np.float16)
+        vc[b, :, pos] = new[:, (Hq + Hkv) * D:].reshape(n, Hkv, D).astype(np.float16)
+        at = [i for i, r in enumerate(rows) if off[b] <= r < off[b] + n]
+        t = np.array([rows[i] - off[b] for i in at], int)
+        if not at:
+            continue
+        L = pos0[b] + n
+        o, e = attend(rotated(new[t, :Hq * D], pos[t], Hq), kc[b, :, :L].transpose(1, 0, 2).astype(np.float64),
+                      vc[b, :, :L].transpose(1, 0, 2).astype(np.float64), pos[t])
+        out[at], bound[at] = o.reshape(len(at), -1), e.reshape(len(at), -1)
+    return out, bound, kc, vc
+
+
+def test_uncut_sums_over_the_longest_cache():
+    """Tiles that are not cut along 131072 keys, of values with a mean: nothing of
+    what the sums lose cancels.  A product of sixteen keys may cut 2^-23 off its
+    sum, and a sum has 64 blocks' 512 of them, so 2^-14 of the result at most,
+    systematically; the outputs' roundings, of 128 means, add three times
+    2^-11 / sqrt(3 x 128) to the mean error."""
+    Hq, Hkv, C, n = 64, 1, 1 << 17, 1300
+    rng = np.random.default_rng(4)
+    mean = rng.uniform(0.5, 2.0, D)
+    p = C - n
+    kc = rng.normal(0, 1, (1, Hkv, C, D)).astype(np.float16)
+    vc = (mean + rng.normal(0, 0.1, (1, Hkv, C, D))).astype(np.float16)
+    qkv = rng.normal(0, 1, (n, (Hq + 2) * D))
+    qkv[:, :Hq * D] *= 0.3
+    qkv[:, -D:] = mean + 0.1 * qkv[:, -D:]
+    args = qkv.astype(np.float16), np.array([0, n], np.int32), np.array([p], np.int32), kc, vc
+    got, _, _ = _run(*args, Hq, Hkv)
+    assert sq.sq_check() == 0
+    rows = [0, n - 1]
+    ref, bound, _, _ = _some_rows(args, [n], [p], Hq, Hkv, rows)
+    _assert(got[rows], ref, bound + 2.0 ** -14 * np.abs(ref))
+    bias = ((got[rows].astype(np.float64) - ref) / ref).mean()
+    assert abs(bias) <= 2.0 ** -14 + 3 * 2.0 ** -11 / (3 * 128) ** 0.5, bias
