@@ -338,6 +338,25 @@ def _some_rows(args, lens, pos0, Hq, Hkv, rows):
     return out, bound, kc, vc
 
 
+@pytest.mark.parametrize("lens,pos0,C", [([3000], [0], 3008), ([700, 1, 1500, 333], [0, 900, 257, 2000], 2400),
+                                         ([1300, 1201], [3000, 17], 4304)])
+def test_ctas_that_take_several_items_of_many_blocks(lens, pos0, C):
+    """More tiles than pieces that the plan would cut (40 / 8 heads), three and
+    more of many blocks for each CTA in turn: some rows of every sequence, its
+    first and last among them."""
+    Hq, Hkv = 40, 8
+    args = _case(len(lens), lens, pos0, Hq, Hkv, C)
+    got, k, v = _run(*args, Hq, Hkv)
+    assert sq.sq_check() == 0
+    rng = np.random.default_rng(1)
+    rows = sorted(set(rng.integers(0, sum(lens), 40)) | set(args[1][:-1]) | set(args[1][1:] - 1))
+    ref, bound, rk, rv = _some_rows(args, lens, pos0, Hq, Hkv, rows)
+    assert np.array_equal(k.view(np.uint16), rk.view(np.uint16))
+    assert np.array_equal(v.view(np.uint16), rv.view(np.uint16))
+    _assert(got[rows], ref, bound)
+    assert np.array_equal(got.view(np.uint16), _run(*args, Hq, Hkv)[0].view(np.uint16))
+
+
 def test_uncut_sums_over_the_longest_cache():
     """Tiles that are not cut along 131072 keys, of values with a mean: nothing of
     what the sums lose cancels.  A product of sixteen keys may cut 2^-23 off its
