@@ -15,6 +15,7 @@
 #include "sq_packed.cuh"
 #include "sq_tcgen.cuh"
 
+#include <algorithm>
 #include <mutex>
 #include <stddef.h>
 #include <type_traits>
@@ -1345,12 +1346,21 @@ static bool k4_long(int64_t heads, int64_t Q, int64_t max_ctx) {
 }
 
 // CTAs that share the keys of a group of queries: as many as fill the SMs, at
-// least a step of 32 keys for each of a CTA's warps.
+// least a step of 32 keys for each of a CTA's warps, and at most kK4MaxSteps:
+// mma.sync cuts off what it adds to a sum where an fp32 addition rounds, and the
+// codes' part of the values does not cancel as the values do.  1024 steps in one
+// sum (64 sequences of 131072, 40 / 8 heads) were off by 1.2e-3 of the result;
+// 96 are as many products as attention_kv4_tc_kernel adds up.
+constexpr int kK4MaxSteps = 96;
+static int64_t k4_least(int64_t max_ctx) {
+  constexpr int64_t keys = (int64_t)kK4MaxSteps * kK4Warps * kK4Keys;
+  return (max_ctx + keys - 1) / keys;
+}
 static int64_t k4_shares(int64_t groups, int64_t max_ctx) {
   const int64_t steps = (max_ctx + kK4Keys - 1) / kK4Keys;
   int64_t S = kK4PerSm * (int64_t)device_sm_count() / groups;
   if (S > (steps + kK4Warps - 1) / kK4Warps) S = (steps + kK4Warps - 1) / kK4Warps;
-  return S < 1 ? 1 : S;
+  return std::max(S, k4_least(max_ctx));
 }
 
 size_t attention_kv4_workspace_bytes(int B, int T, int Hq, int Hkv, int64_t max_ctx) {
@@ -1364,7 +1374,8 @@ size_t attention_kv4_workspace_bytes(int B, int T, int Hq, int Hkv, int64_t max_
 
 // Up to 16 shares meet in a cluster (one launch) as long as all clusters are
 // resident; a long cache under few heads takes more, which meet through the
-// workspace and a second launch, from eight steps a warp on.
+// workspace and a second launch, from eight steps a warp on, and so do those of
+// many long caches (k4_least).
 template <int R>
 static cudaError_t launch_kv4_inst(KV4AttnArgs a, cudaStream_t st) {
   const int Z = (a.Q + 8 * R - 1) / (8 * R);
@@ -1382,6 +1393,10 @@ static cudaError_t launch_kv4_inst(KV4AttnArgs a, cudaStream_t st) {
       if (n >= groups) break;
     }
     a.cluster = S > 1;
+    if (S < k4_least(a.max_ctx)) {  // not that many at once: through the workspace
+      S = k4_least(a.max_ctx);
+      a.cluster = 0;
+    }
   }
   a.nsplit = (int)S;
   cudaLaunchConfig_t cfg = {};

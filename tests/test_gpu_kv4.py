@@ -319,3 +319,27 @@ def test_long_caches_keep_their_precision(T, Hq, Hkv, ctx):
     got = out.float().cpu().numpy().astype(np.float64)
     rel = np.linalg.norm(got - ref.reshape(T, -1)) / np.linalg.norm(ref)
     assert rel <= 2.8e-4 * (2 ** 0.5 + 0.5), rel
+
+
+@pytest.mark.parametrize("T", [1, 3])
+def test_many_long_caches_keep_their_precision(T):
+    """As many sequences as leave a (sequence, head) one CTA: what sums over
+    131072 keys lose is a fifth of the outputs' and the weights' rounding (as a
+    whole 2.8e-4, see test_sums_over_many_tiles_keep_their_precision) at most."""
+    B, Hq, Hkv, C = 160, 10, 2, 1 << 17
+    if torch.cuda.mem_get_info()[0] < 2 * B * Hkv * C * 136:
+        pytest.skip("not enough memory")
+    rng = np.random.default_rng(T)
+    cache, vals = _random_cache(rng, 1, Hkv, C, [C - T], T)
+    qkv = rng.normal(0, 1, (T, (Hq + 2 * Hkv) * D)).astype(np.float16)
+    dc = [_t(c).repeat(B, 1, 1, 1) for c in cache]
+    out = torch.empty(B * T, Hq * D, dtype=torch.float16, device=dev())
+    _attention(np.tile(qkv, (B, 1)), B, T, Hq, Hkv, [C - T] * B, dc, out)
+    assert sq.sq_check() == 0
+    pos = C - T + np.arange(T)
+    q = oracle.rope(qkv[:, :Hq * D].astype(np.float64), pos, Hq, D, THETA).reshape(T, Hq, D)
+    ref = oracle.attention(q, vals[0][0].transpose(1, 0, 2), vals[1][0].transpose(1, 0, 2), pos).reshape(T, -1)
+    got = out.float().cpu().numpy().astype(np.float64).reshape(B, T, -1)
+    assert (got == got[:1]).all()
+    rel = np.linalg.norm(got[0] - ref) / np.linalg.norm(ref)
+    assert rel <= 2.8e-4 * 1.2, rel
