@@ -408,8 +408,19 @@ def _check_heads(Hq: int, Hkv: int) -> int:
 
 
 @functools.lru_cache(maxsize=256)
+def _size_on(device: int, name: str, *args) -> int:
+    return int(getattr(load(), name)(*args))
+
+
+def _device_size(name: str, *args) -> int:
+    """A size that goes by the current device's SM count, remembered for each device."""
+    if torch.cuda.is_initialized():
+        return _size_on(torch.cuda.current_device(), name, *args)
+    return int(getattr(load(), name)(*args))
+
+
 def sq_attention_prompt_workspace_bytes(B, N, Hq, Hkv, max_ctx) -> int:
-    return int(load().sq_attention_prompt_workspace_bytes(B, N, Hq, Hkv, 128, max_ctx))
+    return _device_size("sq_attention_prompt_workspace_bytes", B, N, Hq, Hkv, 128, max_ctx)
 
 
 def sq_attention_prompt(qkv, offsets, Hq, Hkv, pos0, theta, k_cache, v_cache, out, workspace,
@@ -464,9 +475,8 @@ def sq_kv4_unpack(k_codes, k_params, v_codes, v_params, first, last, k_cache, v_
     _check("sq_kv4_unpack", load().sq_kv4_unpack(kc, kp, vc, vp, B, Hkv, 128, C, lo, hi, k, v, _stream(stream)))
 
 
-@functools.lru_cache(maxsize=256)
 def sq_attention_kv4_workspace_bytes(B, T, Hq, Hkv, max_ctx) -> int:
-    return int(load().sq_attention_kv4_workspace_bytes(B, T, Hq, Hkv, 128, max_ctx))
+    return _device_size("sq_attention_kv4_workspace_bytes", B, T, Hq, Hkv, 128, max_ctx)
 
 
 def sq_attention_kv4(qkv, B, T, Hq, Hkv, pos0, theta, k_codes, k_params, v_codes, v_params, out, workspace,

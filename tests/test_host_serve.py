@@ -117,6 +117,23 @@ def test_workspace_sizes(lib):
     assert sq.sq_attention_kv4_workspace_bytes(2, 40, 12, 2, 256) == 0
 
 
+@pytest.mark.parametrize("name", ["sq_attention_prompt_workspace_bytes", "sq_attention_kv4_workspace_bytes"])
+def test_workspace_sizes_are_the_current_device_s(monkeypatch, name):
+    """Sizes go by the SMs of the device: another one's answer is not given again."""
+    device = [0]
+
+    class Lib:
+        def __getattr__(self, _):
+            return lambda *args: 1000 + device[0]
+
+    monkeypatch.setattr(sq, "load", Lib)
+    monkeypatch.setattr(torch.cuda, "is_initialized", lambda: True)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: device[0])
+    args = (7, 11, 12, 2, 4242 * 16)  # (asked nowhere else: a remembered size would outlive the test)
+    for device[0] in (0, 1, 0):
+        assert getattr(sq, name)(*args) == 1000 + device[0]
+
+
 def _cpu(*shape, dtype=torch.float16):
     return torch.zeros(*shape, dtype=dtype)
 
