@@ -353,11 +353,13 @@ __global__ void __launch_bounds__(kPrPrepThreads) prompt_prepare_kernel(
     reinterpret_cast<uint4*>(dst + u * 8)[0] = y1;
     reinterpret_cast<uint4*>(dst + u * 8)[8] = y2;
   }
-  // values: 16 lanes a head's row
-  for (int idx = tid; idx < R * Hkv * 16; idx += kPrPrepThreads) {
-    const int i = idx / (Hkv * 16), r = idx - i * (Hkv * 16), h = r >> 4, u = r & 15;
+  // values: 16 lanes a head's row (whole warps go round together, as they vote: one row
+  // of an odd number of heads leaves the last half of one without a part)
+  const int parts = R * Hkv * 16;
+  for (int idx = tid; idx - (tid & 31) < parts; idx += kPrPrepThreads) {
+    const int at = min(idx, parts - 1), i = at / (Hkv * 16), r = at - i * (Hkv * 16), h = r >> 4, u = r & 15;
     const int64_t row = row0 + i;
-    const bool mine = seq[i] >= 0 && pos[i] >= 0;
+    const bool mine = idx < parts && seq[i] >= 0 && pos[i] >= 0;
     uint4 x = make_uint4(0, 0, 0, 0);
     if (mine) {
       x = reinterpret_cast<const uint4*>(qkv + row * width + (int64_t)(Hq + Hkv + h) * kHeadDim)[u];

@@ -154,6 +154,25 @@ def test_what_lies_behind_a_token_has_no_effect():
     sq.sq_check()
 
 
+@pytest.mark.parametrize("lens,Hkv", [([1], 3), ([2, 3], 3), ([1], 1), ([4], 17), ([600, 500], 5)])
+def test_odd_numbers_of_key_value_heads(lens, Hkv):
+    """Rows of values that end in the middle of a warp, with one that is not
+    finite in the last head of the first token."""
+    Hq, C = 2 * Hkv, 608
+    args = _case(Hkv, lens, [0] * len(lens), Hq, Hkv, C)
+    ref, bound, rk, rv = prompt(args[0], lens, [0] * len(lens), args[1], Hq, Hkv, args[3], args[4])
+    args[0][0, -3] = np.inf
+    rv[0, -1, 0, -3] = np.inf
+    got, k, v = _run(*args, Hq, Hkv)
+    assert sq.sq_check() == 0
+    assert np.array_equal(k.view(np.uint16), rk.view(np.uint16))
+    assert np.array_equal(v.view(np.uint16), rv.view(np.uint16))
+    sees = got[:lens[0]].reshape(lens[0], Hq, D)[:, -2:, -3]
+    assert np.isposinf(sees).all()
+    sees[:] = ref[:lens[0]].reshape(lens[0], Hq, D)[:, -2:, -3]
+    _assert(got, ref, bound)
+
+
 def test_a_prompt_in_chunks_equals_the_whole():
     """Chunks behind their own prefix leave the caches of the whole prompt, bit for bit."""
     Hq, Hkv, C, n = 28, 4, 512, 400
