@@ -51,7 +51,6 @@ struct PromptWork {
   unsigned int* done;  // [groups, Hkv, 2] pieces that have arrived
   uint8_t* odd;        // [Hkv, N] a value of this row is not finite
   float* rec;          // partial results: [record, Hkv, 2][kPrRec]
-  float* aside;        // sums put aside: [CTA, 2][kPrRec]
 };
 // m, l and the weighted values of 128 rows, a row's next value 128 floats on
 constexpr int kPrRec = (kHeadDim + 2) * 128;
@@ -417,6 +416,7 @@ struct PromptArgs {
   const PromptWork* work;
   const __half* vc;
   __half* out;
+  float* aside;  // sums put aside: [CTA, 2][kPrRec]
   int Hq, Hkv, G;
   int64_t N, max_ctx;
 };
@@ -468,7 +468,9 @@ __device__ __forceinline__ int pr_blocks(const PromptItem& it, int G, int h) {
 // other is in its softmax.  TMEM: S0, S1, O0, O1, 128 columns each.
 // The running maximum of a row is let lag by up to 2^kPrSlack before O and the
 // sum are rescaled (the result is the same but for fp16's range), so that O
-// leaves TMEM once, at the end, and every kPrSum blocks before it.
+// leaves TMEM once, at the end, and (Long) every kPrSum blocks before it.  Long is
+// for caches of more than kPrSum blocks: its code, though not run, made a call of 20
+// tokens take 12.5 us instead of 11.9.
 // Bound: the chain of a half's block (scores, softmax, weights, products), as its
 // scores have one place.  8000 tokens, 40 / 8 heads: 485 us, 1.35 PFLOP/s, the
 // tensor pipe busy for 59 % of them; 1.83 us for both halves' block, 1.06 of them
@@ -476,6 +478,7 @@ __device__ __forceinline__ int pr_blocks(const PromptItem& it, int G, int h) {
 // weights are) cost 735 us for the call instead of 541: twice the hand-overs, and
 // products of 64 columns; sixteen softmax warps 554; exponentials of the first 64
 // keys before the block's maximum is known 547.
+template <bool Long>
 __global__ void __launch_bounds__(kPrThreads, 1)
     prompt_attention_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk,
                             const __grid_constant__ CUtensorMap tv, const PromptArgs a) {
@@ -625,7 +628,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
 #pragma unroll
               for (int kk = 4 * half; kk < 4 * half + 4; ++kk)
                 tc_mma_f16_ts(tmem + 256 + h * 128, tmem + h * 128 + kk * 8, vd + kk * (16 * 128 / 16), id_pv,
-                              j % kPrSum > 0 || kk > 0);
+                              (Long ? j % kPrSum : j) > 0 || kk > 0);
             }
             if (!fine) break;
             ++np[h];
@@ -727,8 +730,8 @@ __global__ void __launch_bounds__(kPrThreads, 1)
         if (j > 0) pr_wait(PR_BAR(o_done) + 8 * (h), (ns & 1u) ^ 1u, s);
         __syncwarp();
         tc_fence_after();
-        if (j % kPrSum == 0 && j > 0) {  // (this block's products begin a sum, once its weights are there)
-          float* aside = a.work->aside + ((int64_t)blockIdx.x * 2 + h) * kPrRec + row;
+        if (Long && j % kPrSum == 0 && j > 0) {  // (this block's products begin a sum, once its weights are there)
+          float* aside = a.aside + (int)(blockIdx.x * 2 + h) * kPrRec + row;
           const float2 lp = f2unpack(l2);
           float f = 0.0f, la = lp.x + lp.y;
           l2 = 0;
@@ -740,16 +743,16 @@ __global__ void __launch_bounds__(kPrThreads, 1)
           __stcg(aside + kHeadDim * 128, m);
           __stcg(aside + (kHeadDim + 1) * 128, la);
 #pragma unroll 1
-          for (int i = 0; i < 4; ++i) {
-            uint32_t o[32];
-            tm_ld32(to + 32 * i, o);
+          for (int i = 0; i < kHeadDim; i += 16) {
+            uint32_t o[16];
+            tm_ld16(to + i, o);
             tm_wait_ld();
-            tm_loaded32(o);
+            tm_loaded16(o);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
+            for (int e = 0; e < 16; ++e) {
               float x = __uint_as_float(o[e]);
-              if (j > kPrSum) x = fmaf(f, __ldcg(aside + (32 * i + e) * 128), x);
-              __stcg(aside + (32 * i + e) * 128, x);
+              if (j > kPrSum) x = fmaf(f, __ldcg(aside + (i + e) * 128), x);
+              __stcg(aside + (i + e) * 128, x);
             }
           }
         }
@@ -791,7 +794,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
           const float mn = fmaxf(m, mb);
           const float f = m == -INFINITY ? 0.0f : ex2((m - mn) * c);
           m = mn;
-          if (j % kPrSum > 0) {
+          if (Long ? j % kPrSum > 0 : j > 0) {
             const unsigned long long f2 = f2pack(f, f);
             asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(l2) : "l"(f2));
 #pragma unroll 1
@@ -834,11 +837,23 @@ __global__ void __launch_bounds__(kPrThreads, 1)
       tc_fence_after();
       const float2 lp = f2unpack(l2);
       float l = lp.x + lp.y, fa = 0.0f;
-      const float* aside = a.work->aside + ((int64_t)blockIdx.x * 2 + h) * kPrRec + row;
-      if (nb > kPrSum) {
+      if (Long && nb > kPrSum) {
+        const float* aside = a.aside + (int)(blockIdx.x * 2 + h) * kPrRec + row;
         const float ma = __ldcg(aside + kHeadDim * 128);
         if (ma != -INFINITY) fa = ex2((ma - m) * c);
         l = fmaf(__ldcg(aside + (kHeadDim + 1) * 128), fa, l);
+#pragma unroll 1
+        for (int i = 0; i < kHeadDim; i += 16) {
+          uint32_t o[16];
+          tm_ld16(to + i, o);
+          tm_wait_ld();
+          tm_loaded16(o);
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            o[e] = __float_as_uint(fmaf(fa, __ldcg(aside + (i + e) * 128), __uint_as_float(o[e])));
+          tm_st16(to + i, o);
+        }
+        tm_wait_st();
       }
       const bool split = it.nsplit > 1;
       const float f = split ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
@@ -852,11 +867,6 @@ __global__ void __launch_bounds__(kPrThreads, 1)
           tm_ld32(to + 32 * i, o);
           tm_wait_ld();
           tm_loaded32(o);
-        }
-        if (nb > kPrSum) {
-#pragma unroll
-          for (int e = 0; e < 32; ++e)
-            o[e] = __float_as_uint(fmaf(fa, __ldcg(aside + (32 * i + e) * 128), __uint_as_float(o[e])));
         }
 #pragma unroll
         for (int e = 0; e < 32; ++e) o[e] = nb > 0 ? __float_as_uint(__uint_as_float(o[e]) * f) : 0u;
@@ -970,8 +980,10 @@ static cudaError_t prompt_ready() {
   if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   std::lock_guard<std::mutex> lock(mu);
   if (!ready[dev]) {
-    e = cudaFuncSetAttribute(prompt_attention_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPrSmem);
-    if (e != cudaSuccess) return e;
+    for (auto* k : {prompt_attention_kernel<false>, prompt_attention_kernel<true>}) {
+      e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kPrSmem);
+      if (e != cudaSuccess) return e;
+    }
     ready[dev] = true;
   }
   return cudaSuccess;
@@ -999,18 +1011,17 @@ cudaError_t launch_prompt(const __half* qkv, const Packed& pk, int Hq, int Hkv, 
   a.init.done = reinterpret_cast<unsigned int*>(w + l.done);
   a.init.odd = w + l.odd;
   a.init.rec = reinterpret_cast<float*>(w + l.rec);
-  a.init.aside = reinterpret_cast<float*>(w + l.aside);
   const int rows = pk.N <= kPrFewRows ? 1 : 2;
   e = launch_pdl(rows == 1 ? prompt_prepare_kernel<1> : prompt_prepare_kernel<2>,
                  dim3((unsigned)((pk.N + rows - 1) / rows + 1)), dim3(kPrPrepThreads), 0, st, qkv, Hq,
                  rope_freq(theta), a, kc, vc, qr, out);
   if (e != cudaSuccess) return e;
-  PromptArgs p = {a.work, vc, out, Hq, Hkv, a.G, pk.N, pk.max_ctx};
+  PromptArgs p = {a.work, vc, out, reinterpret_cast<float*>(w + l.aside), Hq, Hkv, a.G, pk.N, pk.max_ctx};
   int64_t grid = (pk.N * a.G / kPrRows + pk.B) * Hkv;
   if (l.max_recs > grid) grid = l.max_recs;
   if (grid > a.sms) grid = a.sms;
-  return launch_pdl(prompt_attention_kernel, dim3((unsigned)grid), dim3(kPrThreads), (size_t)kPrSmem, st, tq, tk, tv,
-                    p);
+  return launch_pdl(pk.max_ctx > kPrSum * kPrKeys ? prompt_attention_kernel<true> : prompt_attention_kernel<false>,
+                    dim3((unsigned)grid), dim3(kPrThreads), (size_t)kPrSmem, st, tq, tk, tv, p);
 }
 
 cudaError_t take_prompt_status(uint32_t* bits) {
