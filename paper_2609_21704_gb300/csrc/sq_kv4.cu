@@ -396,13 +396,14 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
   }
 
   float o[16][4], m[R], l[R], zl[R];
-  float vcap = 0.0f, vup = 1.0f;  // value scales up to vcap; vup brings them to 2^9
+  float vcap[R], vup[R];  // scales of the values a query sees: up to vcap; vup brings them to 2^9
 #pragma unroll
   for (int i = 0; i < 16; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     m[r] = -INFINITY;
-    l[r] = zl[r] = 0.0f;
+    l[r] = zl[r] = vcap[r] = 0.0f;
+    vup[r] = 1.0f;
   }
 
   for (int it = 0; step < s1; ++it, step += kK4Warps) {
@@ -410,7 +411,7 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
     __syncwarp();  // the parameters are other lanes' copies
     const uint8_t* sl = slot0 + (it % kK4Stages) * kK4Stage;
     const bool edge = (step + 1) * kK4Keys > p0 + 1;
-    float sc[R][4][2], mx[R], vm = 0.0f;
+    float sc[R][4][2], mx[R], vm[R];
     {
       // scores: four columns' tiles of eight keys, two chains of products at a time
       float s[4][4];
@@ -476,31 +477,49 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
         }
     }
 #pragma unroll
-    for (int r = 0; r < R; ++r) mx[r] = -INFINITY;
+    for (int r = 0; r < R; ++r) {
+      mx[r] = -INFINITY;
+      vm[r] = 0.0f;
+    }
 #pragma unroll
     for (int n = 0; n < 4; ++n)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        vm = fmaxf(vm, ws[n][e]);
+        vm[0] = fmaxf(vm[0], ws[n][e]);
 #pragma unroll
         for (int r = 0; r < R; ++r) mx[r] = fmaxf(mx[r], sc[r][n][e]);
       }
-    bool grown = vm > vcap;
+    if (R > 1) {
+      vm[R - 1] = vm[0];
+      if (edge) {  // (of the rows that each of the two queries sees)
 #pragma unroll
-    for (int r = 0; r < R; ++r) grown = grown || mx[r] - m[r] > 5.0f;
-    if (__any_sync(0xffffffffu, grown)) {
-      float fv = 1.0f;
-      vm = warp_max(vm);
-      if (vm > vcap) {
-        // the power of two above vm becomes 2^9: weights up to 2^5 stay below 2^15
-        const float cap = __uint_as_float(((__float_as_uint(vm) >> 23) + 1) << 23);
-        const float up = 512.0f / cap;
-        fv = up / vup;
-        vcap = cap;
-        vup = up;
+        for (int r = 0; r < R; ++r) {
+          vm[r] = 0.0f;
+#pragma unroll
+          for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              if (step * kK4Keys + 8 * n + 2 * t4 + e <= lim[r]) vm[r] = fmaxf(vm[r], ws[n][e]);
+        }
       }
+    }
+    bool grown = false;
+#pragma unroll
+    for (int r = 0; r < R; ++r) grown = grown || vm[r] > vcap[r] || mx[r] - m[r] > 5.0f;
+    if (__any_sync(0xffffffffu, grown)) {
 #pragma unroll
       for (int r = 0; r < R; ++r) {
+        float fv = 1.0f;
+        vm[r] = fmaxf(vm[r], __shfl_xor_sync(0xffffffffu, vm[r], 1));
+        vm[r] = fmaxf(vm[r], __shfl_xor_sync(0xffffffffu, vm[r], 2));
+        if (vm[r] > vcap[r]) {
+          // the power of two above vm becomes 2^9: weights up to 2^5 stay below 2^15
+          const float cap = __uint_as_float(((__float_as_uint(vm[r]) >> 23) + 1) << 23);
+          const float up = 512.0f / cap;
+          fv = up / vup[r];
+          vcap[r] = cap;
+          vup[r] = up;
+        }
         mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 1));
         mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 2));
         const float mn = fmaxf(m[r], mx[r]);
@@ -531,7 +550,7 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
         for (int e = 0; e < 2; ++e) {
           const float p = k4_ex2(sc[r][n][e] - mm);
           l[r] += p;
-          float w = ws[n][e] * vup, wlow = wl[n][e];
+          float w = ws[n][e] * vup[r], wlow = wl[n][e];
           // (a row that the one query sees and the other does not may hold a NaN)
           if (R > 1 && edge && sc[r][n][e] == -INFINITY) w = wlow = 0.0f;
           const float x = p * w;
@@ -573,9 +592,9 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
 
   // ---- records (m, l, -, -, o[D]) over the ring: a warp's, then the CTA's
   float* rec = reinterpret_cast<float*>(k4_smem + C::kOffRing);
-  const float down = 1.0f / vup;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
+    const float down = 1.0f / vup[r];
 #pragma unroll
     for (int i = 1; i < 4; i <<= 1) {
       l[r] += __shfl_xor_sync(0xffffffffu, l[r], i);
@@ -725,11 +744,13 @@ constexpr int kT4Stages = 3;
 constexpr int kT4Codes = kT4Keys * 64, kT4Stage = 2 * kT4Codes + 2 * kT4Keys * 4;
 constexpr int kT4OffS = kT4OffC + kT4Stages * kT4Stage;
 struct T4Shared {
-  float m[kT4Max], fac[kT4Max];  // running maxima (units of log 2); what sums are rescaled by
+  float m[kT4Max], fac[kT4Max];  // running maxima (units of log 2); what sums of weights are rescaled by
+  float cap[kT4Max], up[kT4Max], fo[kT4Max];  // scales of the values a query sees: up to cap; up brings
+                                              // them to 2^9; what sums of values are rescaled by
   alignas(16) float neg[kT4Max];
   alignas(16) float qsum[kT4Max];
   int lim[kT4Max];               // the last position a query sees
-  float wm[4][kT4Max], wv[4];    // maxima of the warps: scores, value scales
+  float wm[4][kT4Max], wv[4][kT4Max];  // maxima of the warps: scores, value scales
   float total[2][kT4Max];
   int amax;                      // largest finite |query value|, as bits
   uint64_t c_full[kT4Stages], c_empty[kT4Stages], k_full[2], v_full[2], s_full[2], p_ready[2], pv_done[2], drain;
@@ -872,6 +893,8 @@ __global__ void __launch_bounds__(kT4Threads, 1) attention_kv4_tc_kernel(const K
           s->lim[i] = p0 + (q0 + i) % T;
           s->m[i] = -INFINITY;
           s->neg[i] = INFINITY;
+          s->cap[i] = 0.0f;
+          s->up[i] = 1.0f;
         }
       }
     }
@@ -1019,7 +1042,7 @@ __global__ void __launch_bounds__(kT4Threads, 1) attention_kv4_tc_kernel(const K
     unsigned long long l2[N / 2], z2[N / 2];
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) l2[i] = z2[i] = 0;
-    float vcap = 0.0f, vup = 1.0f;  // value scales up to vcap; vup brings them to 2^9
+    float vcap = 0.0f, vup = 1.0f;  // every query's before the first position that one does not see
     for (int t = 0; t < n; ++t) {
       const int p = t & 1, key = (t0 + t) * kT4Keys + tid;  // (below 2^17)
       const bool edge = (t0 + t + 1) * kT4Keys - 1 > first;
@@ -1083,24 +1106,39 @@ __global__ void __launch_bounds__(kT4Threads, 1) attention_kv4_tc_kernel(const K
           const int o = __reduce_max_sync(0xffffffffu, x ^ ((x >> 31) & 0x7fffffff));
           if (lane == 0) s->wm[warp][i] = __int_as_float(o ^ ((o >> 31) & 0x7fffffff));
         }
-        const float vw = warp_max(w);
-        if (lane == 0) s->wv[warp] = vw;
+        // of value scales the largest that each query sees: up to this lane's key, then its own
+        float vw = fmaxf(w, 0.0f);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const float x = __shfl_up_sync(0xffffffffu, vw, o);
+          if (lane >= o) vw = fmaxf(vw, x);
+        }
+#pragma unroll
+        for (int i0 = 0; i0 < N; i0 += 32) {
+          const int i = min(i0 + lane, N - 1), last = s->lim[i] - (key - lane);
+          const float x = __shfl_sync(0xffffffffu, vw, min(max(last, 0), 31));
+          s->wv[warp][i] = last < 0 ? 0.0f : x;
+        }
         named_bar_sync(1, 128);
+        // the power of two above vm becomes 2^9: weights up to 2^5 stay below 2^15
+        auto power = [](float vm, float& cap, float& up) {
+          if (!(vm > cap)) return 1.0f;
+          const float old = up;
+          cap = __uint_as_float(((__float_as_uint(vm) >> 23) + 1) << 23);
+          up = 512.0f / cap;
+          return up / old;
+        };
+        auto largest = [&](int i) { return fmaxf(fmaxf(s->wv[0][i], s->wv[1][i]), fmaxf(s->wv[2][i], s->wv[3][i])); };
         if (tid < N) {
           const float mo = s->m[tid];
           const float mn = fmaxf(mo, fmaxf(fmaxf(s->wm[0][tid], s->wm[1][tid]), fmaxf(s->wm[2][tid], s->wm[3][tid])));
           s->m[tid] = mn;
           s->neg[tid] = -mn;
-          s->fac[tid] = mo == -INFINITY ? 0.0f : ex2(mo - mn);
+          const float f = mo == -INFINITY ? 0.0f : ex2(mo - mn);
+          s->fac[tid] = f;
+          s->fo[tid] = f * power(largest(tid), s->cap[tid], s->up[tid]);
         }
-        const float vm = fmaxf(fmaxf(s->wv[0], s->wv[1]), fmaxf(s->wv[2], s->wv[3]));
-        float fv = 1.0f;
-        if (vm > vcap) {  // the power of two above vm becomes 2^9: weights up to 2^5 stay below 2^15
-          const float cap = __uint_as_float(((__float_as_uint(vm) >> 23) + 1) << 23), up = 512.0f / cap;
-          fv = up / vup;
-          vcap = cap;
-          vup = up;
-        }
+        if (!edge) power(largest(0), vcap, vup);
         named_bar_sync(1, 128);
         if (t > 0) {
           tc_wait(T4_BAR(pv_done) + 8 * (p ^ 1), ((t - 1) >> 1) & 1, &s->dead, &g_kv4_status);
@@ -1108,14 +1146,14 @@ __global__ void __launch_bounds__(kT4Threads, 1) attention_kv4_tc_kernel(const K
           tc_fence_after();
 #pragma unroll 1
           for (int k = 0; k < min(t, kT4Sums); ++k)
-#pragma unroll
+#pragma unroll 1
             for (int i = 0; i < N; i += 16) {
               uint32_t o[16];
               tm_ld16(to + 64 * k + i, o);
               tm_wait_ld();
               tm_loaded16(o);
 #pragma unroll
-              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * (s->fac[i + e] * fv));
+              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * s->fo[i + e]);
               tm_st16(to + 64 * k + i, o);
             }
 #pragma unroll
@@ -1149,7 +1187,7 @@ __global__ void __launch_bounds__(kT4Threads, 1) attention_kv4_tc_kernel(const K
             if constexpr (apart.value) {
               const bool s0 = a0 != -INFINITY, s1 = a1 != -INFINITY;
               z2[j] = ffma2_to(pr, f2pack(s0 ? wl : 0.0f, s1 ? wl : 0.0f), z2[j]);
-              h[e] = pack_f16x2(s0 ? x0 * ws : 0.0f, s1 ? x1 * ws : 0.0f);
+              h[e] = pack_f16x2(s0 ? x0 * (w * s->up[2 * j]) : 0.0f, s1 ? x1 * (w * s->up[2 * j + 1]) : 0.0f);
             } else {
               z2[j] = ffma2_to(pr, wl2, z2[j]);
               h[e] = pack_f16x2(x0 * ws, x1 * ws);
@@ -1186,7 +1224,6 @@ __global__ void __launch_bounds__(kT4Threads, 1) attention_kv4_tc_kernel(const K
         red[(N + 2 * i) * 129 + tid] = y.x;
         red[(N + 2 * i + 1) * 129 + tid] = y.y;
       }
-      const float down = 1.0f / vup;
       const int d = 16 * (tid & 7) + (tid >> 3);  // this TMEM lane's dimension
 #pragma unroll
       for (int i = 0; i < N; i += 16) {
@@ -1203,7 +1240,7 @@ __global__ void __launch_bounds__(kT4Threads, 1) attention_kv4_tc_kernel(const K
           for (int e = 0; e < 16; ++e) x[e] += __uint_as_float(o[e]);
         }
 #pragma unroll
-        for (int e = 0; e < 16; ++e) rows[(i + e) * 129 + d] = x[e] * down;
+        for (int e = 0; e < 16; ++e) rows[(i + e) * 129 + d] = x[e] * (s->cap[i + e] * (1.0f / 512.0f));
       }
       tc_fence_before();
       named_bar_sync(1, 128);

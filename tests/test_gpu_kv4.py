@@ -343,3 +343,32 @@ def test_many_long_caches_keep_their_precision(T):
     assert (got == got[:1]).all()
     rel = np.linalg.norm(got[0] - ref) / np.linalg.norm(ref)
     assert rel <= 2.8e-4 * 1.2, rel
+
+
+@pytest.mark.parametrize("T,G,C,p", [(5, 1, 64, 20), (5, 7, 64, 20), (9, 1, 64, 20), (5, 7, 65536, 20),
+                                     (24, 2, 65536, 115), (32, 4, 65536, 100)])
+def test_a_value_that_a_query_does_not_see_has_no_part_in_its_precision(T, G, C, p):
+    """The last token's value is of fp16's whole range, 6e7 times the others' size
+    (in each of the three kernels, and where new tokens lie in two tiles).  The
+    queries before it: as a whole within the bound of long caches above."""
+    rng = np.random.default_rng(T + G)
+    cache, vals = _random_cache(rng, 1, 1, C, [p], T)
+    v = rng.normal(0, 1e-3, (1, 1, C, D))
+    v[:, :, p + T - 1] = np.where(np.arange(D) % 2, 6e4, -6e4)
+    cv, pv = kv4_encode(v.astype(np.float16))
+    vals[1] = kv4_value(cv, pv)
+    pv[:, :, p + T:] = np.nan
+    cache[2:] = [kv4_pack_v(cv).reshape(1, 1, C, 64), pv]
+    qkv = rng.normal(0, 1, (T, (G + 2) * D)).astype(np.float16)
+    out = torch.empty(T, G * D, dtype=torch.float16, device=dev())
+    _attention(qkv, 1, T, G, 1, [p], [_t(c) for c in cache], out)
+    assert sq.sq_check() == 0
+    pos, L = p + np.arange(T), p + T
+    q = oracle.rope(qkv[:, :G * D].astype(np.float64), pos, G, D, THETA).reshape(T, G, D)
+    ref = oracle.attention(q, vals[0][0, :, :L].transpose(1, 0, 2), vals[1][0, :, :L].transpose(1, 0, 2), pos)
+    got = out.float().cpu().numpy().astype(np.float64).reshape(T, G, D)
+    rel = np.linalg.norm(got - ref, axis=(1, 2)) / np.linalg.norm(ref, axis=(1, 2))
+    assert rel[:-1].max() <= 2.8e-4 * (2 ** 0.5 + 0.5), rel
+    # the last one's result is one weight times that value: its rounding to fp16 is no mean
+    # over mantissas but 2^-11 at most, alike in every element, and the output's adds as much
+    assert rel[-1] <= 2 * 2.0 ** -11, rel
