@@ -190,6 +190,87 @@ def test_4_bit_caches_of_any_length(stack, params):
     assert _compare(g.tokens(), params, prompts, 1) > 0
 
 
+def _rows_of(cache, li, b, n):
+    """(keys, values, half a step of each) of the first n positions that a 4-bit cache holds."""
+    kc, kp, vc, vp = (c[b].cpu().numpy() for c in cache.kv4[li])
+    pairs = vc.reshape(vc.shape[0], -1, 128)
+    by = np.empty((pairs.shape[0], 2 * pairs.shape[1], 64), np.uint8)
+    for odd in (0, 1):
+        for byte in (0, 1):
+            by[:, odd::2, byte::2] = pairs[..., 2 * odd + byte::4]
+    out = []
+    for codes, par in ((kc, kp), (by, vp)):
+        c = np.empty(codes.shape[:2] + (128,))
+        c[..., 0::2], c[..., 1::2] = codes & 15, codes >> 4
+        par = par.astype(np.float64)
+        out += [(c * par[..., :1] + par[..., 1:])[:, :n].transpose(1, 0, 2), par[:, :n, :1].transpose(1, 0, 2) / 2]
+    return out[0], out[2], out[1], out[3]
+
+
+def _step_over(params, cache, b, token, p):
+    """The decoder of the oracle for one token at position p over the rows of a
+    4-bit cache, its own among them: its logits; every layer's row of the cache
+    has to be this token's key and value within half a step, and as much for a
+    dozen roundings to fp16 on the way as 12 x 2^-11 of the row's largest value."""
+    Hq, Hkv, D = params["q_heads"], params["kv_heads"], params["head_dim"]
+    x = np.asarray(params["embed"], np.float64)[[token]]
+    pos = np.array([p])
+    for li, (w_qkv, w_o, w_gu, w_dn) in enumerate(params["layers"]):
+        qkv = O.linear(O.rmsnorm(x, params["gamma"][2 * li], params["eps"]), w_qkv)
+        q = O.rope(qkv[:, :Hq * D], pos, Hq, D, params["theta"])
+        k = O.rope(qkv[:, Hq * D:(Hq + Hkv) * D], pos, Hkv, D, params["theta"]).reshape(Hkv, D)
+        v = qkv[:, (Hq + Hkv) * D:].reshape(Hkv, D)
+        ks, vs, dk, dv = _rows_of(cache, li, b, p + 1)
+        for got, want, half in ((ks[p], k, dk[p]), (vs[p], v, dv[p])):
+            assert (np.abs(got - want) <= half + 12 * 2.0 ** -11 * np.abs(want).max()).all(), (b, p, li)
+        a = O.attention(q.reshape(1, Hq, D), ks, vs, pos)
+        x = x + O.linear(a.reshape(1, Hq * D), w_o)
+        h = O.rmsnorm(x, params["gamma"][2 * li + 1], params["eps"])
+        x = x + O.linear(O.silu_gate_rows(O.linear(h, w_gu), params["intermediate"]), w_dn)
+    return O.linear(O.rmsnorm(x, params["gamma"][-1], params["eps"]), params["lm_head"])[0]
+
+
+@pytest.mark.parametrize("K,max_ctx", [(0, 96), (0, 70), (3, 120)])
+def test_each_step_over_the_parents_4_bit_cache(stack, params, K, max_ctx):
+    """Steps of one token and verify passes of four, the first eager, the others
+    replayed: every token's row in every layer, and the tokens that follow from
+    attention over these rows, where the two largest logits are clear."""
+    prompts, s, steps = _prompts(), torch.cuda.Stream(), 12 if K == 0 else 5
+    g = Generator(stack, len(prompts), K, max(LENS), max_ctx, verifier_kv="int4")
+    g.prefill_packed(prompts, s)
+    g.run(steps, s)
+    s.synchronize()
+    assert g.status() == 0
+    logits = g.tv.logits.float().cpu().numpy()
+    sure = checked = 0
+    for b, (t, prompt) in enumerate(zip(g.tokens(), prompts)):
+        assert t[:len(prompt)] == prompt and len(t) >= len(prompt) + 1 + steps
+        for p in range(len(prompt), len(t) - 1):
+            z = _step_over(params, g.tv, b, t[p], p)
+            order = np.argsort(-z, kind="stable")
+            if z[order[0]] - z[order[1]] > GAP_TOL:
+                assert t[p + 1] == order[0], (b, p)
+                sure += 1
+            checked += 1
+        if K == 0:
+            assert np.abs(logits[b] - z).max() <= GAP_TOL
+    assert checked >= len(prompts) * steps and sure >= checked * 3 // 4
+
+
+def test_drafts_over_a_4_bit_cache_are_accepted(stack):
+    """What is generated is the parent's whatever the draft's cache holds; its
+    drafts are accepted about as often as those over an fp16 cache (from a wrong
+    cache they agree with the parent's by chance, one in a thousand)."""
+    prompts, s, got = _prompts([9, 14, 5, 11], seed=21), torch.cuda.Stream(), []
+    for kv in ("fp16", "int4"):
+        g = Generator(stack, len(prompts), 3, 14, 160, draft_kv=kv)
+        g.prefill_packed(prompts, s)
+        g.run(10, s)
+        assert g.status() == 0
+        got.append(sum(len(t) - len(p) - 1 - 10 for t, p in zip(g.tokens(), prompts)))
+    assert got[0] > 20 and got[1] >= got[0] / 2, got
+
+
 def test_a_4_bit_pass_without_scratch_is_refused(stack):
     cache, st = DecoderState(stack, 1, 1, 16, kv="int4"), PromptState(stack, 4, 1, 16)
     with pytest.raises(ValueError):
