@@ -429,14 +429,16 @@ SQ_API sq_status sq_spec_drafts(const int32_t* samples, const int32_t* last2, in
  *   out[row] = sum_{j <= pos} p_j v_j / sum_j p_j,
  *   p_j = exp(q . k_j / sqrt(D))
  * over the cache, query head h against key/value head h / (Hq / Hkv), out
- * fp16 [N, Hq * D].  Rotated keys are rounded to fp16 once, correctly,
- * rotated queries once, from fp32; products are exact; sums and the softmax's
- * statistics are fp32, of values and probabilities on the tensor core, which cuts
- * off where an fp32 addition rounds (over any length 2^-14 of the result at
- * most, where nothing cancels); a probability relative to its row's maximum is
- * rounded to fp16 for its product with the value (its sum is not).  What lies in the caches behind a
- * token's position, infinities and NaN included, has no effect on its row;
- * scores of -inf have no weight, and a row without any other is zero.  A sequence
+ * fp16 [N, Hq * D].  A rotated key x1 c - x2 s (x2 c + x1 s) is rounded to
+ * fp16 once, to the nearest value unless it lies within 2^-33 (|x1| + |x2|) of
+ * the middle between two; a rotated query once, from fp32.  Products are exact;
+ * sums and the softmax's statistics are fp32, but the tensor core, which adds up
+ * scores and weighted values, cuts off where an fp32 addition rounds (of the
+ * weighted values 2^-14 at most over any length, where nothing cancels).  A
+ * probability relative to its row's maximum is rounded to fp16 for its product
+ * with the value (its sum is not).  What lies in the caches behind a token's
+ * position, infinities and NaN included, has no effect on its row; scores of
+ * -inf have no weight, and a row without any other is zero.  A sequence
  * that does not fit its cache (pos0[b] < 0 or pos0[b] + length > max_ctx)
  * writes nothing to it, gets zero rows and sets SQ_DEV_BAD_POSITION; offsets
  * that decrease or leave [0, N] set it too, and nothing at all is written.
@@ -453,12 +455,12 @@ SQ_API sq_status sq_attention_prompt(const void* qkv, int64_t N, const int32_t* 
 /* ------------------------------------------------------------------------
  * The key/value cache in four bits (Sec. III-A keeps the variants' weights in
  * 4 and 8 bits; the paper leaves the caches open).  A row is one position of
- * one key/value head: 128 fp16 values x, of a key after its rotation, which
- * is rounded to fp16 once, correctly.  With lo = min x and hi = max x,
+ * one key/value head: 128 fp16 values x, of a key after its rotation, rounded
+ * as by sq_attention_prompt.  With lo = min x and hi = max x,
  *   s = fp16((hi - lo) / 15), 2^-24 if that is zero and hi > lo,
  *   c = clamp(rint((x - lo) / s), 0, 15) (ties to even), 0 if s = 0,
  * every step rounded to fp32; the row stands for c * s + lo.  Codes and
- * parameters are bit-identical to this definition.
+ * parameters of x are bit-identical to this definition.
  *   k_codes  uint8 [B, Hkv, max_ctx, 64]: byte i holds dimension 2i in its
  *            low half and 2i + 1 in its high half
  *   v_codes  uint8 [B, Hkv, max_ctx / 2, 128]: per pair of positions, bytes
@@ -480,11 +482,17 @@ SQ_API sq_status sq_attention_prompt(const void* qkv, int64_t N, const int32_t* 
  *   continues behind.  first[b] < 0 or last[b] > max_ctx (and first < last)
  *   writes nothing for b and sets SQ_DEV_BAD_POSITION.
  * sq_attention_kv4: sq_attention over these caches (same arguments, layouts
- *   and limits; the new tokens already appended): fp32 accumulation over
- *   exact codes, out fp16; above eight queries a key/value head, (Hq / Hkv) *
- *   T > 8, a weight relative to its row's maximum is rounded to fp16 for its
- *   product with the codes, as in sq_attention_prompt.  Rows behind a query's position have no effect,
- *   whatever they hold.  A sequence with pos0[b] < 0 or pos0[b] + T > max_ctx
+ *   and limits; the new tokens already appended), out fp16.  Queries are two
+ *   fp16 terms (22 bits), products with codes exact.  Their sums are fp32, but
+ *   the tensor core cuts off where an fp32 addition rounds; it adds up at most
+ *   24 tiles of 128 keys, or 96 steps of 32, and these sums are added by fp32
+ *   additions.  A weight relative to its row's maximum, times its value's scale,
+ *   is two fp16 terms for up to eight queries a key/value head; above, (Hq /
+ *   Hkv) * T > 8, it is rounded to fp16 once, as in sq_attention_prompt (so a
+ *   pass over several tokens may round what a step of one does not).  Either way
+ *   it is kept to within 2^-33 of the largest value scale that the query sees.
+ *   Rows behind a query's position have no part in its result, whatever they
+ *   hold.  A sequence with pos0[b] < 0 or pos0[b] + T > max_ctx
  *   gets zero rows and sets SQ_DEV_BAD_POSITION.  workspace:
  *   sq_attention_kv4_workspace_bytes(...) bytes, 16-byte aligned, no
  *   zero-fill; calls sharing one must not overlap on the GPU. */

@@ -140,7 +140,10 @@ __device__ __forceinline__ float2 kv4_params(const __half* p, int64_t slot) {
 }
 
 // One CTA per 32 positions of a (sequence, head); a thread two neighbouring
-// positions' eight dimensions of keys and values, 16-byte stores side by side.
+// positions' eight dimensions of keys and values, 16-byte stores side by side.  5493
+// rows of 8 heads: 9.4 us, 4.2 by their bytes; what is written stays in L2 (DRAM 8 %
+// busy), and it is bound by instructions (issue 55 %) and the chain of a thread's loads.
+// The grid is the caches' capacity (CTAs outside a range end at once).
 constexpr int kUnpackRows = 32;
 __device__ __forceinline__ uint32_t kv4_half2(uint32_t nibbles, float2 p) {
   // 2^23 + n, less 2^23
@@ -277,8 +280,9 @@ __device__ __forceinline__ void k4_cluster_sync() {
 // R = 2: sixteen queries, rows of their own; queries are two terms (two products),
 // a weight relative to its row's maximum is rounded to fp16 (as in
 // sq_attention_prompt: with a second term half of the products would be its).
-// The running maximum may lag by 2^5 before sums are rescaled, and so may the
-// power of two that brings weights times value scales into fp16's range.
+// The running maximum may lag by 2^5 before sums are rescaled.  A power of two, of
+// the largest value scale that a query sees, brings weights times value scales into
+// fp16's range (steps of 2^-24, against 2^8 to 2^9 for that scale at a weight of one).
 // Bound: the products, 96 a step (R = 2; 64 with R = 1) of 16 cycles on each quarter
 // of an SM: 456 CTAs over 30000 keys take 196 ns a step of an SM, 150 with R = 1,
 // with two CTAs an SM 213 and 162; two or four CTAs' worth of registers and 3 to 9
@@ -720,7 +724,7 @@ __global__ void __launch_bounds__(kK4Threads, 3) attention_kv4_kernel(const KV4A
 // where the four warps agree.  One thread issues the products.
 // attention_kv4_kernel converts a code for every sixteen queries and is bound by
 // mma.sync, 16 cycles an m16n8k16 on each quarter of an SM: 16 x 5 tokens behind
-// 30000, 28 / 4 heads, 282 us.  Here 155, 1.2 us a tile.  What that is made of (taken
+// 30000, 28 / 4 heads, 282 us.  Here 152, 1.2 us a tile.  What that is made of (taken
 // with three rounds of CTAs, 163 us in all): without copies, conversion and softmax
 // 140, with a third of the products besides 105; the rest are hand-overs (weights
 // written, products, their place free).  Two places for the weights and two tiles of

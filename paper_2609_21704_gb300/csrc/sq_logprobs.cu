@@ -11,9 +11,10 @@
 // groups' maxima can be among the `top` largest: threads that met one in a
 // sixteenth of their part read that again (out of L2), and what passes, some tens
 // of entries, is ranked by counting.
-// Bound: instructions for many rows, 14 an entry (1000 rows of 152064, five
-// alternatives: 83 us, 3.7 TB/s, issue 72 % busy); for one row the chain of its
-// cluster's three meetings (151936 entries: 7.6 us, 10.4 with five alternatives).
+// Bound: instructions for many rows, 14 an entry, of which the steps written here need
+// about six (1000 rows of 152064, five alternatives: 83 us, 3.7 TB/s, issue 72 % busy);
+// for one row the chain of its cluster's three meetings (151936 entries: 7.6 us, 10.4
+// with five alternatives).
 #include "sq_serve.h"
 
 #include <mutex>

@@ -337,7 +337,11 @@ __global__ void __launch_bounds__(kPrPrepThreads) prompt_prepare_kernel(
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float p = __half2float(e1[e]), q = __half2float(e2[e]);
-      if (h < Hq) {  // queries: fp32 does (one in 5000 to the other fp16 neighbour)
+      // queries: fp32 does (one in 5000 to the other fp16 neighbour).  They are operands of
+      // the tensor core, which takes fp16 beside the caches' fp16 keys; a second term for
+      // what the rounding leaves would double the scores' products, half of all.  With the
+      // weights' rounding the result is off by 2.2e-4 to 2.9e-4, by 1.9e-4 to 2.1e-4 without
+      if (h < Hq) {
         const float2 c = csq[i][e * 8 + u];
         z1[e] = __float2half_rn(p * c.x - q * c.y);
         z2[e] = __float2half_rn(q * c.x + p * c.y);
@@ -532,7 +536,8 @@ __global__ void __launch_bounds__(kPrThreads, 1)
   };
 
   // registers: 384 threads x 168 at launch; the softmax groups take 208, the
-  // others keep 88 (256 x 208 + 128 x 88 = 384 x 168); with 72 those spilled
+  // others keep 88 (256 x 208 + 128 x 88 = 384 x 168); with 72 those spilled in
+  // their loops (with 88 the kernel still spills 64 bytes, Long 84)
   if (warp >= 8) {
    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
    if (warp == 8) {
