@@ -399,3 +399,31 @@ def test_uncut_sums_over_the_longest_cache():
     _assert(got[rows], ref, bound + 2.0 ** -14 * np.abs(ref))
     bias = ((got[rows].astype(np.float64) - ref) / ref).mean()
     assert abs(bias) <= 2.0 ** -14 + 3 * 2.0 ** -11 / (3 * 128) ** 0.5, bias
+
+
+@pytest.mark.parametrize("n,p,Hq,Hkv", [(1300, 11000, 64, 1), (1200, 58000, 10, 2)])
+def test_sums_put_aside_and_what_changes_between_them(n, p, Hq, Hkv):
+    """Tiles of 75 to 100 blocks, uncut and as pieces of a cut tile, whose running
+    maxima grow along the keys (up to six times as long as normal ones: scores'
+    fp32 sums lose six times as much, a share of at most one of the values), with
+    a value of a new token infinite and one of another NaN."""
+    C = (p + n + 15) // 16 * 16
+    rng = np.random.default_rng(p)
+    kc, vc = (rng.standard_normal((1, Hkv, C, D), np.float32) for _ in range(2))
+    kc *= np.linspace(0.1, 6.0, C, dtype=np.float32)[:, None]
+    qkv = rng.normal(0, 1, (n, (Hq + 2 * Hkv) * D)).astype(np.float16)
+    args = qkv, np.array([0, n], np.int32), np.array([p], np.int32), kc.astype(np.float16), vc.astype(np.float16)
+    rows = [0, 257, 700, n - 1]
+    ref, bound, _, _ = _some_rows(args, [n], [p], Hq, Hkv, rows)
+    bound += 5 * 2.0 ** -13 * np.abs(args[4].astype(np.float32)).max()
+    got, _, _ = _run(*args, Hq, Hkv)
+    assert sq.sq_check() == 0
+    _assert(got[rows], ref, bound)
+    w = (Hq + Hkv) * D
+    qkv[200, w + 3] = np.inf
+    qkv[600, w + 9] = np.nan
+    odd, _, _ = _run(*args, Hq, Hkv)
+    odd, got = (x.reshape(n, Hkv, Hq // Hkv, D) for x in (odd, got))
+    assert np.isposinf(odd[200:, 0, :, 3]).all() and np.isnan(odd[600:, 0, :, 9]).all()
+    odd[200:, 0, :, 3], odd[600:, 0, :, 9] = got[200:, 0, :, 3], got[600:, 0, :, 9]
+    assert np.array_equal(odd, got)
